@@ -164,7 +164,8 @@ def _linear(s):
 def _codes(v, t):
     """The values that the codes of the rows of v stand for, and the scales."""
     a = v.abs().amax(dim=1, keepdim=True)
-    inverse, scale = 127.0 / a, a / 127.0
+    top = torch.full_like(a, 127.0)     # tensors on both sides of a division: a plain number's reciprocal would be multiplied by
+    inverse, scale = top / a, a / top
     q = torch.floor(v.double() * inverse.double() + 0.5).clamp(-127, 127).float()
     return (q * scale).to(t), scale[:, 0]
 
@@ -249,8 +250,8 @@ def work(case):
 # ------------------------------------------------------------------ the definition, in 64 bits
 
 def _exact_codes(v):
-    peak = v.abs().max(dim=1).values.float()
-    i, scale = (127.0 / peak).double(), (peak / 127.0).double()
+    peak = v.abs().max(dim=1).values.float().double()
+    i, scale = (127.0 / peak).float().double(), (peak / 127.0).float().double()
     return (v * i.unsqueeze(1) + 0.5).floor().clamp(min=-127, max=127) * scale.unsqueeze(1), scale
 
 
