@@ -83,7 +83,8 @@ typedef enum {
 } f8_status;
 
 typedef enum { F8_U8 = 0, F8_S8 = 1, F8_S32 = 2,
-               F8_S32_RELU = 3      /* output of the sibling entry points only: int32, max(value, 0) */
+               F8_S32_RELU = 3,     /* output of the sibling entry points only: int32, max(value, 0) */
+               F8_F32 = 4, F8_F16 = 5, F8_BF16 = 6      /* real values: the entry points with scales per row only */
 } f8_dtype;
 
 /*
@@ -333,6 +334,100 @@ f8_status f8_fold_quantize_fixed(const f8_fold_desc *desc, const float *w, const
 size_t f8_format_study_workspace_bytes(void);
 f8_status f8_format_study_fixed(const float *x, long long n, int is_unsigned, double *err, int *best_fl,
                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* ---------------------------------------------------------------- 8-bit products of real-valued tensors */
+
+/* The paper multiplies 8-bit codes whose formats are powers of two, one per tensor.  A transformer's linear layers multiply the
+ * same codes, but take their scales from the data: one real scale per token (row of activations) and one per output channel (row
+ * of weights).  The four entry points below are that path: rows of real values to codes, the product of codes, the norms and the
+ * residual sum between two blocks, and what is asked of the logits at the end.
+ *
+ * Conventions beside those at the head of this file
+ *   - Real tensors are F8_F32, F8_F16 or F8_BF16; all arithmetic on them is in 32 bits and rounded once, when it is stored.
+ *   - A matrix has unit stride along a row; ld* is the distance of its rows in elements (0: dense), positive and at least the row's
+ *     length.  Pointers need the alignment of their element only; rows that start at multiples of 16 bytes are read and
+ *     written in wide words, others in narrower ones, with the same result.  No gap between rows is written.
+ *   - A row's codes: with a = max |v| over the row, s = a / 127 and i = 127 / a, both rounded to 32 bits,
+ *         q = floor(v * i + 1/2) in [-127, 127]       (the product exact: round half up as everywhere in this library)
+ *     and the value a code stands for is q * s.  A row with a < 2^-100 is a row of zeros: s = 0, q = 0.  A row that holds an
+ *     infinity or a NaN has s = a / 127 (so infinite or NaN) and q = 0: each of its values, and each product made of it, is NaN.
+ *   - An output may be the memory of an input of the same size of element and the same row distance (in place); other overlaps of
+ *     outputs with inputs or with each other are not allowed.
+ *   - Nothing is kept from call to call, no memory is allocated, and every call can be captured into a graph (f8_linear_scaled: after
+ *     one call on that device outside a capture, which allocates the status word of f8_device_status). */
+
+/* y = x w^T with scales:  acc = sum_k x[i, k] * w[j, k]  exact in int32;
+ *     y[i, j] = round( fma( (float)acc * x_scale[i], w_scale[j], bias[j] ) )       float arithmetic, one rounding per operation
+ *   x [n, k] F8_U8 or F8_S8, w [out, k] int8; x_scale [x_scales], x_scales n or 1 (one scale for all rows); w_scale [w_scales],
+ *   w_scales out or 1; bias [out] of bias_dtype or NULL; y [n, out] of y_dtype (F8_F32, F8_F16, F8_BF16).
+ * Errors: F8_ERR_NULL, F8_ERR_SHAPE, F8_ERR_DTYPE, F8_ERR_ALIGN (element alignment), F8_ERR_ACC_BOUND (k * 255 * 128, or
+ * k * 128 * 128 for signed x, reaches 2^31), F8_ERR_TIMEOUT. */
+typedef struct {
+    int n, k, out;
+    int x_dtype, y_dtype, bias_dtype;
+    int x_scales, w_scales;
+    long long ldx, ldw, ldy;
+} f8_scaled_desc;
+f8_status f8_linear_scaled(const f8_scaled_desc *desc, const void *x, const float *x_scale, const int8_t *w, const float *w_scale,
+                           const void *bias, void *y, void *cuda_stream);
+
+/* Rows of real values to codes, v = act(x) * u (u NULL: act(x)): the activations in front of a product, with the gate of a gated block
+ * (u the other half of the widened tensor), or a weight matrix, whose rows are output channels.
+ *   x, u [n, c] of dtype; q [n, c] int8 and scale [n], or both NULL; y [n, c] of dtype, or NULL: with q the values that the codes
+ *   stand for, without q the values v themselves.
+ *   act: F8_ACT_NONE v = x; F8_ACT_SILU x / (1 + exp(-x)); F8_ACT_GELU x * (1 + erf(x / sqrt 2)) / 2.
+ * Errors: F8_ERR_NULL (neither q nor y, q without scale), F8_ERR_SHAPE, F8_ERR_DTYPE, F8_ERR_ALIGN, F8_ERR_UNSUPPORTED (act), F8_ERR_TIMEOUT. */
+enum { F8_ACT_NONE = 0, F8_ACT_SILU = 1, F8_ACT_GELU = 2, F8_ACT_SIGMOID = 3, F8_ACT_TANH = 4 };
+typedef struct {
+    long long n;
+    int c, dtype, act;
+    long long ldx, ldu, ldy, ldq;
+} f8_rows_desc;
+f8_status f8_quantize_rows(const f8_rows_desc *desc, const void *x, const void *u, int8_t *q, float *scale, void *y, void *cuda_stream);
+
+/* What lies between two blocks of a transformer, in one pass over its rows:
+ *     t = residual + branch_scale * g(gate) * post(x)      (residual NULL: 0; gate NULL: 1)
+ *     residual_out = t;   v = pre(t)                       (v from t before it is rounded for residual_out)
+ *     q, scale: the codes of v; y: the values the codes stand for, or without q the values v themselves
+ *   post, pre: F8_NORM_NONE: z;  F8_NORM_RMS: z / sqrt(mean(z^2) + eps) * (w + weight_offset) + b;
+ *              F8_NORM_LAYER: the same of z - mean(z).  w NULL: 1 in place of (w + weight_offset); b NULL: 0.
+ *   g: F8_ACT_NONE, F8_ACT_SIGMOID, F8_ACT_TANH.  gate [gate_rows, c], gate_rows n (per token) or 1 (per channel).
+ *   x, gate, residual, residual_out, y [n, c] of dtype; post_w, post_b, pre_w, pre_b [c] of w_dtype (F8_F32 or dtype).
+ *   Any of residual_out, y, (q, scale) may be NULL, not all.
+ * Errors: as f8_quantize_rows; F8_ERR_UNSUPPORTED also for weights of a norm that is F8_NORM_NONE; F8_ERR_SHAPE for an eps
+ * that is negative or not finite, a weight_offset or branch_scale that is not finite. */
+enum { F8_NORM_NONE = 0, F8_NORM_RMS = 1, F8_NORM_LAYER = 2 };
+typedef struct {
+    long long n;
+    int c, dtype, w_dtype;
+    int post_norm, pre_norm, gate_act;
+    long long gate_rows;
+    float eps, weight_offset, branch_scale;
+    long long ldx, ldg, ldr, lds, ldy, ldq;      /* x, gate, residual, residual_out, y, q */
+} f8_norm_desc;
+f8_status f8_norm_quantize(const f8_norm_desc *desc, const void *x, const void *gate, const void *residual, const void *post_w,
+                           const void *post_b, const void *pre_w, const void *pre_b, void *residual_out, int8_t *q, float *scale,
+                           void *y, void *cuda_stream);
+
+/* Log probabilities under z = logits * inv_temperature (F8_S32 logits, such as a network's: codes in format fl, z = code * 2^-fl *
+ * inv_temperature), lse = log sum exp z over a row:
+ *     logprobs[i, t] = z[tokens[i, t]] - lse          entropy[i] = -sum p log p, p = exp(z - lse)
+ *     top_ids[i, 0 .. top), top_logprobs: the largest logits in falling order, equal ones by rising index
+ *   logits [n, v] of dtype F8_S32, F8_F32, F8_F16 or F8_BF16; tokens [n, tokens] int64; logprobs [n, tokens], entropy [n],
+ *   top_logprobs [n, top] float, top_ids [n, top] int64, all dense; any output may be NULL, not all; top <= 32 and <= v.
+ *   A token below 0 is a padded place: its log probability is 0.  One at or beyond v has NaN.  Logits of -infinity have probability 0; a
+ *   row of nothing else has log probabilities of -infinity (its top_ids are 0, 1, ...) and entropy 0.  A row that holds
+ *   a NaN or +infinity has NaN in every log probability and in its entropy; NaN sorts before +infinity.
+ * Errors: F8_ERR_NULL, F8_ERR_SHAPE (also an inv_temperature that is not positive and finite), F8_ERR_DTYPE, F8_ERR_FL_RANGE (fl outside
+ * [-8, 32]), F8_ERR_ALIGN, F8_ERR_TIMEOUT. */
+typedef struct {
+    long long n;
+    int v, dtype, fl, tokens, top;
+    float inv_temperature;
+    long long ldl;
+} f8_logprobs_desc;
+f8_status f8_token_logprobs(const f8_logprobs_desc *desc, const void *logits, const int64_t *tokens, float *logprobs, float *entropy,
+                            float *top_logprobs, int64_t *top_ids, void *cuda_stream);
 
 /* ---------------------------------------------------------------- diagnostics */
 

@@ -8,6 +8,7 @@ module fails if the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -28,6 +29,9 @@ _lib = ctypes.CDLL(_LIB_PATH)
 
 F8_OK = 0
 F8_U8, F8_S8, F8_S32, F8_S32_RELU = 0, 1, 2, 3
+F8_F32, F8_F16, F8_BF16 = 4, 5, 6
+F8_ACT_NONE, F8_ACT_SILU, F8_ACT_GELU, F8_ACT_SIGMOID, F8_ACT_TANH = 0, 1, 2, 3, 4
+F8_NORM_NONE, F8_NORM_RMS, F8_NORM_LAYER = 0, 1, 2
 STATUS_NAMES = ["F8_OK", "F8_ERR_NULL", "F8_ERR_SHAPE", "F8_ERR_DTYPE", "F8_ERR_FL_RANGE", "F8_ERR_SHIFT_RANGE",
                 "F8_ERR_ALIGN", "F8_ERR_ACC_BOUND", "F8_ERR_WORKSPACE", "F8_ERR_UNSUPPORTED", "F8_ERR_CUDA",
                 "F8_ERR_TIMEOUT"]
@@ -218,6 +222,160 @@ def f8_requantize_dual_fixed(acc, fa, y1, y1_dtype, fl_y1, y2=None, y2_dtype=F8_
     """int32 tensor in format fa -> one or two 8-bit tensors, each with its own fractional length (Sec. 4.3)."""
     _check(_lib.f8_requantize_dual_fixed(acc.numel(), _ptr(acc), fa, _ptr(y1), y1_dtype, fl_y1, _ptr(y2), y2_dtype, fl_y2,
                                          _stream(stream)))
+
+
+# ------------------------------------------------------------------ 8-bit products of real-valued tensors
+
+class ScaledDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n", "k", "out", "x_dtype", "y_dtype", "bias_dtype", "x_scales", "w_scales")] + \
+               [(n, ctypes.c_longlong) for n in ("ldx", "ldw", "ldy")]
+
+
+class RowsDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("c", "dtype", "act")] + \
+               [(n, ctypes.c_longlong) for n in ("ldx", "ldu", "ldy", "ldq")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("c", "dtype", "w_dtype", "post_norm", "pre_norm", "gate_act")] + \
+               [("gate_rows", ctypes.c_longlong)] + [(n, ctypes.c_float) for n in ("eps", "weight_offset", "branch_scale")] + \
+               [(n, ctypes.c_longlong) for n in ("ldx", "ldg", "ldr", "lds", "ldy", "ldq")]
+
+
+class LogprobsDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("v", "dtype", "fl", "tokens", "top")] + \
+               [("inv_temperature", ctypes.c_float), ("ldl", ctypes.c_longlong)]
+
+
+_lib.f8_linear_scaled.argtypes = [_vp] * 8
+_lib.f8_quantize_rows.argtypes = [_vp] * 7
+_lib.f8_norm_quantize.argtypes = [_vp] * 13
+_lib.f8_token_logprobs.argtypes = [_vp] * 8
+
+_CODES = {torch.uint8: F8_U8, torch.int8: F8_S8, torch.int32: F8_S32, torch.float32: F8_F32, torch.float16: F8_F16, torch.bfloat16: F8_BF16}
+_REAL = (torch.float32, torch.float16, torch.bfloat16)
+
+
+def _bad(what: str):
+    raise ValueError(what)
+
+
+def _matrix(t: torch.Tensor, what: str, shape=None, dtypes=None, device: int = -1):
+    """(pointer, row distance) of a matrix with unit stride along its rows, checked against a shape, its types and a device."""
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        _bad(f"{what}: a matrix{' of shape ' + str(tuple(shape)) if shape is not None else ''} is needed, got {tuple(t.shape)}")
+    if dtypes is not None and t.dtype not in dtypes:
+        _bad(f"{what}: type {t.dtype} where one of {dtypes} is needed")
+    if t.get_device() < 0 or (device >= 0 and t.get_device() != device):
+        _bad(f"{what}: on {t.device}, not on the current CUDA device")
+    rows, cols = t.shape
+    step, unit = t.stride()
+    if rows > 0x7fffffff or cols > 0x7fffffff:
+        _bad(f"{what}: extents beyond 2^31 - 1")
+    if (unit != 1 and cols > 1) or (step < cols and rows > 1):
+        _bad(f"{what}: rows with unit stride that do not overlap are needed, got strides {t.stride()}")
+    return t.data_ptr(), step if rows > 1 else max(step, cols)
+
+
+def _vector(t: Optional[torch.Tensor], what: str, sizes, dtypes, device: int):
+    """Pointer of a dense vector (any shape with that many elements)."""
+    if t is None:
+        return None
+    if t.numel() not in sizes or t.dtype not in dtypes:
+        _bad(f"{what}: {sizes} elements of one of {dtypes} are needed, got {t.numel()} of {t.dtype}")
+    if t.get_device() != device or not t.is_contiguous():
+        _bad(f"{what}: a dense tensor on the current CUDA device is needed")
+    return t.data_ptr()
+
+
+def _device() -> int:
+    return _get_device() if _get_device is not None else torch.cuda.current_device()
+
+
+# Descriptors by what is in them: building one takes longer than the rest of a call.
+_scaled_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(ScaledDesc(*a)))
+_rows_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(RowsDesc(*a)))
+_norm_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(NormDesc(*a)))
+_logprobs_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(LogprobsDesc(*a)))
+_F32, _S8, _I64, _XCODES, _LOGITS = (torch.float32,), (torch.int8,), (torch.int64,), (torch.uint8, torch.int8), (torch.int32,) + _REAL
+
+
+def f8_linear_scaled(x, x_scale, w, w_scale, y, bias=None, stream=None):
+    """y = x w^T of 8-bit codes, one real scale per row of x (or one for all) and per row of w (or one for all).
+
+    x [n, k] uint8 or int8, w [out, k] int8, x_scale [n] or [1], w_scale [out] or [1] float32, bias [out] or None, y [n, out]
+    float32, float16 or bfloat16; rows may be strided.
+    """
+    dev = _device()
+    xp, ldx = _matrix(x, "x", None, _XCODES, dev)
+    wp, ldw = _matrix(w, "w", None, _S8, dev)
+    n, k = x.shape
+    out = w.shape[0]
+    if w.shape[1] != k:
+        _bad(f"w: rows of {k} codes are needed, got {w.shape[1]}")
+    yp, ldy = _matrix(y, "y", (n, out), _REAL, dev)
+    xs, ws, bp = _vector(x_scale, "x_scale", (n, 1), _F32, dev), _vector(w_scale, "w_scale", (out, 1), _F32, dev), _vector(bias, "bias", (out,), _REAL, dev)
+    d = _scaled_desc(n, k, out, _CODES[x.dtype], _CODES[y.dtype], _CODES[bias.dtype] if bias is not None else F8_F32,
+                     x_scale.numel(), w_scale.numel(), ldx, ldw, ldy)
+    _check(_lib.f8_linear_scaled(d, xp, xs, wp, ws, bp, yp, _stream(stream)))
+
+
+def f8_quantize_rows(x, q=None, scale=None, y=None, u=None, act=F8_ACT_NONE, stream=None):
+    """Rows of act(x) * u to int8 codes q [n, c] with scale [n]; y: the values the codes stand for (without q: act(x) * u itself)."""
+    dev = _device()
+    xp, ldx = _matrix(x, "x", None, _REAL, dev)
+    shape, t = x.shape, (x.dtype,)
+    n, c = shape
+    up, ldu = _matrix(u, "u", shape, t, dev) if u is not None else (None, 0)
+    yp, ldy = _matrix(y, "y", shape, t, dev) if y is not None else (None, 0)
+    qp, ldq = _matrix(q, "q", shape, _S8, dev) if q is not None else (None, 0)
+    _check(_lib.f8_quantize_rows(_rows_desc(n, c, _CODES[x.dtype], act, ldx, ldu, ldy, ldq), xp, up, qp,
+                                 _vector(scale, "scale", (n,), _F32, dev), yp, _stream(stream)))
+
+
+def f8_norm_quantize(x, q=None, scale=None, y=None, *, residual=None, residual_out=None, gate=None, gate_act=F8_ACT_NONE,
+                     post_norm=F8_NORM_NONE, post_w=None, post_b=None, pre_norm=F8_NORM_RMS, pre_w=None, pre_b=None, eps=1e-5,
+                     weight_offset=0.0, branch_scale=1.0, stream=None):
+    """t = residual + branch_scale * gate_act(gate) * post(x); residual_out = t; rows of pre(t) to int8 codes q with scale.
+
+    y: the values the codes stand for (without q: pre(t) itself).  gate [n, c] or [1, c]; norm weights [c] float32 or of x's type.
+    """
+    dev = _device()
+    xp, ldx = _matrix(x, "x", None, _REAL, dev)
+    shape, t = x.shape, (x.dtype,)
+    n, c = shape
+    gp, ldg, gate_rows = None, 0, 1
+    if gate is not None:
+        gate_rows = gate.shape[0]
+        gp, ldg = _matrix(gate, "gate", (1 if gate_rows == 1 else n, c), t, dev)
+    rp, ldr = _matrix(residual, "residual", shape, t, dev) if residual is not None else (None, 0)
+    sp, lds = _matrix(residual_out, "residual_out", shape, t, dev) if residual_out is not None else (None, 0)
+    yp, ldy = _matrix(y, "y", shape, t, dev) if y is not None else (None, 0)
+    qp, ldq = _matrix(q, "q", shape, _S8, dev) if q is not None else (None, 0)
+    wt = next((v.dtype for v in (pre_w, post_w, pre_b, post_b) if v is not None), torch.float32)
+    if wt is not torch.float32 and wt is not x.dtype:
+        _bad(f"norm weights of {wt} with rows of {x.dtype}")
+    w = [_vector(v, "norm weights", (c,), (wt,), dev) for v in (post_w, post_b, pre_w, pre_b)]
+    d = _norm_desc(n, c, _CODES[x.dtype], _CODES[wt], post_norm, pre_norm, gate_act, gate_rows, eps, weight_offset, branch_scale,
+                   ldx, ldg, ldr, lds, ldy, ldq)
+    _check(_lib.f8_norm_quantize(d, xp, gp, rp, w[0], w[1], w[2], w[3], sp, qp, _vector(scale, "scale", (n,), _F32, dev), yp, _stream(stream)))
+
+
+def f8_token_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_logprobs=None, top_ids=None, fl=0, inv_temperature=1.0, stream=None):
+    """Log probabilities of given tokens [n, t] (int64; below 0: padding), entropy [n] and the largest alternatives [n, top] of logits [n, v].
+
+    int32 logits are codes with fl fractional bits, as a network's last layer gives them.
+    """
+    dev = _device()
+    lp, ldl = _matrix(logits, "logits", None, _LOGITS, dev)
+    n, v = logits.shape
+    count = 0 if tokens is None else tokens.numel() // max(n, 1)
+    top = max((t.shape[-1] for t in (top_logprobs, top_ids) if t is not None), default=0)
+    d = _logprobs_desc(n, v, _CODES[logits.dtype], fl, count, top, inv_temperature, ldl)
+    _check(_lib.f8_token_logprobs(d, lp, _vector(tokens, "tokens", (n * count,), _I64, dev),
+                                  _vector(logprobs, "logprobs", (n * count,), _F32, dev), _vector(entropy, "entropy", (n,), _F32, dev),
+                                  _vector(top_logprobs, "top_logprobs", (n * top,), _F32, dev),
+                                  _vector(top_ids, "top_ids", (n * top,), _I64, dev), _stream(stream)))
 
 
 def f8_conv_workspace_bytes(desc: ConvDesc) -> int:
@@ -423,6 +581,18 @@ class Net:
         _check(_lib.f8_net_forward(self._h, batch, _ptr(x), _ptr(out), _ptr(workspace), workspace.numel(), dptr,
                                    _stream(stream)))
         return out
+
+    def classify(self, x: torch.Tensor, top: int = 5, stream=None):
+        """(classes, log probabilities), both [batch, top], of the network's 32-bit logits: a forward pass and f8_token_logprobs."""
+        last = self.layers[-1]
+        if last.kind != synth.LINEAR or last.y_dtype != F8_S32:
+            raise ValueError("the network does not end in 32-bit logits")
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
+            logits = self.forward(x)
+            ids = torch.empty((x.shape[0], top), dtype=torch.int64, device=x.device)
+            lp = torch.empty((x.shape[0], top), dtype=torch.float32, device=x.device)
+            f8_token_logprobs(logits, top_logprobs=lp, top_ids=ids, fl=last.fl_x + last.fl_w)
+        return ids, lp
 
     def set_profiling(self, on: bool):
         _check(_lib.f8_net_set_profiling(self._h, 1 if on else 0))

@@ -283,6 +283,7 @@ static f8_status pending_timeout() {
                     "f8_device_status() gives the details and clears the record", v & 0xff, (v >> 8) - 1);
     return F8_OK;
 }
+f8_status f8_pending_timeout() { return pending_timeout(); }
 
 extern "C" {
 

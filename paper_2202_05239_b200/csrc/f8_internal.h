@@ -167,3 +167,6 @@ int *f8_last_plan_info();
 
 // Records a message for f8_last_error() and returns `s` (for entry points defined outside f8_api.cu).
 f8_status f8_set_error(f8_status s, const char *message);
+
+// F8_OK, or F8_ERR_TIMEOUT (with its message) while the record of a wait that a kernel gave up is pending.
+f8_status f8_pending_timeout();

@@ -1,0 +1,77 @@
+// Real-valued rows: element types, block-wide reductions and the rounding of a row to 8-bit codes with one scale, shared by the
+// kernels around 8-bit products.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "f8_internal.h"
+
+namespace {
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+struct SumOp { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct UMaxOp { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; } };
+
+// One value of the whole block, the same in every thread and in every run (fixed order).  `room`: 32 words of shared memory.
+template <int THREADS, typename V, typename Op>
+__device__ __forceinline__ V block_reduce(V v, Op op, V *room) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
+    if (THREADS == 32) return v;
+    constexpr int WARPS = THREADS / 32;
+    __syncthreads();                        // the room may still be read from the reduction before
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = room[0];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) v = op(v, room[w]);
+    return v;
+}
+
+// The bits of |v|: their order as unsigned numbers is the order of the magnitudes, with infinity above all numbers and NaN
+// above infinity, so a maximum over them (unlike one over floats) keeps what is not finite.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Scale of a row's codes and the factor that takes values to codes, from the largest magnitude.
+struct RowScale {
+    float scale, inverse;
+    __device__ __forceinline__ explicit RowScale(uint32_t peak) {
+        const float a = __uint_as_float(peak);
+        const bool zeros = a < 0x1p-100f, finite = peak < 0x7f800000u;
+        scale = zeros ? 0.f : __fdiv_rn(a, 127.f);
+        inverse = zeros || !finite ? 0.f : __fdiv_rn(127.f, a);
+    }
+    // floor(v * inverse + 1/2): the sum is rounded towards -infinity, which no integer lies under, so the floor is that of the exact
+    // sum.  |v * inverse| <= 127 (1 + 2^-23), hence |code| <= 127 without a clip.  NaN (from 0 * infinity) converts to 0.
+    __device__ __forceinline__ int code(float v) const { return __float2int_rd(__fmaf_rd(v, inverse, 0.5f)); }
+};
+
+inline int real_size(int dtype) { return dtype == F8_F32 ? 4 : (dtype == F8_F16 || dtype == F8_BF16 ? 2 : 0); }
+
+// Launch whose blocks may start while what is before them in the stream drains; the kernels wait before they touch memory.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_stream_go_on() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+}   // namespace

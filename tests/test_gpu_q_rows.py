@@ -1,0 +1,274 @@
+"""Rows of real values to codes (f8_quantize_rows) and the step between two blocks (f8_norm_quantize) against their 64-bit forms."""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import Guarded, api
+from scaled_util import U, check_codes, gelu, half_step, norm64, same_codes, silu, strided, tiny
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+SHAPES = [(1, 1), (1, 2), (3, 7), (5, 16), (2, 63), (4, 64), (9, 100), (17, 256), (3, 513), (6, 1024), (2, 1537), (7, 2048), (3, 4100), (2, 8192), (1, 16384), (2, 16385),
+          (1, 40001)]
+
+
+def _values(rng, n, c, t, scale=1.0):
+    return torch.from_numpy(rng.normal(0, scale, size=(n, c))).to(t).cuda()
+
+
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+@pytest.mark.parametrize("n,c", SHAPES)
+def test_plain_rows_have_the_defined_codes(n, c, t):
+    a = api()
+    x = _values(np.random.default_rng(c), n, c, t)
+    q, s, y = Guarded((n, c), torch.int8), Guarded((n,), F32), Guarded((n, c), t)
+    a.f8_quantize_rows(x, q.t, s.t, y=y.t)
+    torch.cuda.synchronize()
+    same_codes(x.float(), q.t, s.t, y.t)
+    assert q.intact() and s.intact() and y.intact()
+    q2, s2 = torch.empty_like(q.t), torch.empty_like(s.t)
+    a.f8_quantize_rows(x, q2, s2)
+    assert torch.equal(q2, q.t) and torch.equal(s2, s.t)
+
+
+@pytest.mark.parametrize("n,c", [(5, 64), (300, 96), (1000, 2048), (513, 4096), (64, 5000)])
+def test_many_rows(n, c):
+    a = api()
+    for t in (BF16, F32):
+        x = _values(np.random.default_rng(n), n, c, t)
+        q, s = torch.empty(n, c, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        a.f8_quantize_rows(x, q, s)
+        same_codes(x.float(), q, s)
+
+
+def test_ties_round_up():
+    """Values on the half step between two codes: the largest magnitude is 127, so a code is the value rounded half up."""
+    a = api()
+    v = torch.tensor([[127.0] + [k + 0.5 for k in range(-127, 127)] + [0.0, -0.0, 0.25, -0.25, np.nextafter(np.float32(0.5), np.float32(0)),
+                                                                      np.nextafter(np.float32(-0.5), np.float32(-1))]], device="cuda", dtype=F32)
+    q, s = torch.empty(v.shape, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+    a.f8_quantize_rows(v, q, s)
+    want = [127] + [k + 1 for k in range(-127, 127)] + [0, 0, 0, 0, 0, -1]
+    assert q[0].tolist() == want and float(s) == 1.0
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n,c", [(1, 1), (3, 7), (9, 100), (4, 1024), (33, 2049), (5, 8192), (2, 20000)])
+def test_activations(n, c, gated, t, act):
+    a = api()
+    rng = np.random.default_rng(c)
+    both = _values(rng, n, 2 * c, t, 3.0)          # gate and value as halves of one tensor, as the widening product leaves them
+    x, u = both[:, :c], both[:, c:] if gated else None
+    q, s, y = torch.empty(n, c, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, c, dtype=t, device="cuda")
+    code = {"silu": a.F8_ACT_SILU, "gelu": a.F8_ACT_GELU}[act]
+    a.f8_quantize_rows(x, q, s, y=y, u=u, act=code)
+    v = (silu if act == "silu" else gelu)(x.double())
+    if gated:
+        v = v * u.double()
+    # the exponential's documented error grows with its argument (2 + 1.2 |x| steps at most, a step 2^-23); the other steps are a handful
+    err = v.abs() * (10 + 2.4 * x.double().abs()) * 2.0 ** -23
+    check_codes(v, err, q, s, y, act)
+    z = torch.empty(n, c, dtype=t, device="cuda")
+    a.f8_quantize_rows(x, y=z, u=u, act=code)       # the values themselves
+    off = (z.double() - v).abs()
+    assert bool((off <= 1.01 * (err + half_step(t) * v.abs()) + tiny(t) + 1e-45).all())
+
+
+def test_activations_far_out():
+    a = api()
+    x = torch.tensor([[-200.0, -100.0, -88.0, -20.0, -5.0, 0.0, 5.0, 88.0, 200.0, 3e38, -3e38]], device="cuda")
+    for act, f in ((a.F8_ACT_SILU, silu), (a.F8_ACT_GELU, gelu)):
+        y = torch.empty_like(x)
+        a.f8_quantize_rows(x, y=y, act=act)
+        want = f(x.double())
+        want = torch.where(x < -1000, torch.zeros_like(want), want)
+        assert bool(torch.isfinite(y).all())
+        assert bool(((y.double() - want).abs() <= want.abs() * (10 + 2.4 * x.double().abs().clamp(max=200)) * 2.0 ** -23 + 1e-37).all()), (y, want)
+
+
+@pytest.mark.parametrize("c", [8, 100, 4096, 20000])
+@pytest.mark.parametrize("t", [BF16, F32])
+def test_zero_tiny_and_not_finite_rows(c, t):
+    a = api()
+    x = _values(np.random.default_rng(1), 8, c, t)
+    x[1] = 0
+    x[2] = 2.0 ** -101
+    x[3, c // 2] = float("inf")
+    x[4, c - 1] = float("nan")
+    x[5, 0] = -float("inf")
+    x[6] *= 1e30 if t == F32 else 1e20
+    q, s, y = torch.full((8, c), 55, dtype=torch.int8, device="cuda"), torch.empty(8, device="cuda"), torch.empty(8, c, dtype=t, device="cuda")
+    a.f8_quantize_rows(x, q, s, y=y)
+    for i in (1, 2):
+        assert float(s[i]) == 0 and not q[i].any() and not y[i].any()
+    for i in (3, 5):
+        assert torch.isinf(s[i]) and not q[i].any() and torch.isnan(y[i]).all()
+    assert torch.isnan(s[4]) and not q[4].any() and torch.isnan(y[4]).all()
+    same_codes(x[[0, 6, 7]].float(), q[[0, 6, 7]], s[[0, 6, 7]], y[[0, 6, 7]])
+
+
+@pytest.mark.parametrize("pad,offset", [(8, 8), (1, 0), (0, 1), (3, 5), (16, 32)])
+@pytest.mark.parametrize("t", [BF16, F32])
+def test_strided_and_unaligned_rows(t, pad, offset):
+    a = api()
+    rng = np.random.default_rng(pad)
+    for n, c in ((4, 96), (3, 1000), (5, 4096)):
+        x, xf = strided(n, c, t, pad, offset, fill=1e4)
+        x.copy_(_values(rng, n, c, t))
+        q, qf = strided(n, c, torch.int8, pad, offset, fill=99)
+        y, yf = strided(n, c, t, pad, offset, fill=99)
+        s = torch.empty(n, device="cuda")
+        a.f8_quantize_rows(x, q, s, y=y)
+        same_codes(x.float(), q, s, y)
+        for flat in (qf, yf):       # nothing between or around the rows is written
+            rest = flat.clone()
+            rest[offset:offset + n * (c + pad)].view(n, c + pad)[:, :c] = 99
+            assert bool((rest == 99).all())
+
+
+@pytest.mark.parametrize("c", [100, 2048, 20001])
+def test_values_in_place(c):
+    a = api()
+    for t in (BF16, F32):
+        x = _values(np.random.default_rng(4), 5, c, t)
+        keep = x.clone()
+        q, s = torch.empty(5, c, dtype=torch.int8, device="cuda"), torch.empty(5, device="cuda")
+        a.f8_quantize_rows(x, q, s, y=x)
+        same_codes(keep.float(), q, s, x)
+
+
+# ------------------------------------------------------------------ the step between two blocks
+
+KINDS = {"none": 0, "rms": 1, "layer": 2}
+
+
+def _step(rng, n, c, t, *, post="none", pre="rms", gate="none", gate_act="none", residual=True, wt=F32, weights=True, bias=False, offset=0.0, beta=1.0,
+          eps=1e-5, codes=True, values=True, total=True, shift=0.0, pad=0, off=0, inplace=False):
+    a = api()
+
+    def rows(scale, mean=0.0, fill=None):
+        v, _ = strided(n, c, t, pad, off, fill=fill)
+        v.copy_((torch.from_numpy(rng.normal(mean, scale, size=(n, c)))).to(t))
+        return v
+    x, r = rows(1.0), rows(2.0, shift) if residual else None
+    g = None if gate == "none" else torch.from_numpy(rng.normal(0, 1, size=(n if gate == "token" else 1, c))).to(t).cuda()
+    vec = lambda m, s: torch.from_numpy(rng.normal(m, s, size=c)).to(wt).cuda()      # noqa: E731
+    post_w = vec(1 - offset, 0.1) if post != "none" and weights else None
+    pre_w = vec(1 - offset, 0.1) if pre != "none" and weights else None
+    post_b = vec(0, 0.1) if post != "none" and bias else None
+    pre_b = vec(0, 0.1) if pre != "none" and bias else None
+    act = {"none": a.F8_ACT_NONE, "sigmoid": a.F8_ACT_SIGMOID, "tanh": a.F8_ACT_TANH}[gate_act]
+    x64, r64 = x.double(), r.double() if residual else torch.zeros(n, c, dtype=torch.float64, device="cuda")
+    z, ze = norm64(x64, torch.zeros_like(x64), KINDS[post], post_w, post_b, offset, eps)
+    if g is not None:
+        g64 = g.double()
+        g64 = torch.sigmoid(g64) if gate_act == "sigmoid" else torch.tanh(g64) if gate_act == "tanh" else g64
+        ze = ze * g64.abs() + (z * g64).abs() * ((10 + 2.4 * g.double().abs()) * 2 * U if gate_act != "none" else 0) + U * (z * g64).abs()
+        z = z * g64
+    t64 = r64 + beta * z
+    te = abs(beta) * ze + U * t64.abs() + abs(beta) * 2.0 ** -24 * z.abs()
+    v, ve = norm64(t64, te, KINDS[pre], pre_w, pre_b, offset, eps)
+
+    q, s = (strided(n, c, torch.int8, pad, off, fill=0)[0], torch.empty(n, device="cuda")) if codes else (None, None)
+    y = strided(n, c, t, pad, off)[0] if values else None
+    so = (r if inplace and residual else strided(n, c, t, pad, off)[0]) if total else None
+    a.f8_norm_quantize(x, q, s, y, residual=r, residual_out=so, gate=g, gate_act=act, post_norm=KINDS[post], post_w=post_w, post_b=post_b,
+                       pre_norm=KINDS[pre], pre_w=pre_w, pre_b=pre_b, eps=eps, weight_offset=offset, branch_scale=beta)
+    torch.cuda.synchronize()
+    if total:
+        over = (so.double() - t64).abs() - 1.01 * (te + half_step(t) * t64.abs()) - tiny(t)
+        assert bool((over <= 0).all()), f"residual sum off by {over.max().item()} more than the bound"
+    if codes:
+        check_codes(v, ve, q, s, y, "step")
+    elif values:
+        over = (y.double() - v).abs() - 1.01 * (ve + half_step(t) * v.abs()) - tiny(t)
+        assert bool((over <= 0).all()), f"values off by {over.max().item()} more than the bound"
+
+
+@pytest.mark.parametrize("post,pre", list(itertools.product(["none", "rms", "layer"], repeat=2)))
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+def test_step(post, pre, gate, t):
+    rng = np.random.default_rng(11)
+    for n, c in ((1, 1), (3, 65), (5, 1537), (2, 4096)):
+        _step(rng, n, c, t, post=post, pre=pre, gate=gate, beta=0.25, bias=pre == "layer")
+
+
+@pytest.mark.parametrize("n,c", SHAPES + [(300, 128), (777, 1537), (260, 3000), (150, 8192)])
+def test_step_shapes(n, c):
+    rng = np.random.default_rng(n + c)
+    _step(rng, n, c, BF16, post="rms", pre="rms", gate="channel", beta=0.5)
+    _step(rng, n, c, F16, pre="layer", bias=True, gate="token")
+
+
+@pytest.mark.parametrize("codes,values,total", [(True, False, True), (True, False, False), (False, True, True), (False, True, False), (False, False, True),
+                                                (True, True, False)])
+@pytest.mark.parametrize("c", [64, 1000, 4096, 20000])
+def test_step_outputs(codes, values, total, c):
+    _step(np.random.default_rng(c), 4, c, BF16, codes=codes, values=values, total=total, post="layer", bias=True)
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "tanh"])
+@pytest.mark.parametrize("gate", ["channel", "token"])
+def test_step_gates(act, gate):
+    for t in (BF16, F32):
+        _step(np.random.default_rng(1), 6, 640, t, gate=gate, gate_act=act, beta=1.5)
+
+
+@pytest.mark.parametrize("kw", [dict(residual=False), dict(weights=False), dict(offset=1.0), dict(wt=BF16), dict(wt=BF16, bias=True, pre="layer"), dict(inplace=True),
+                                dict(shift=300.0, pre="layer", bias=True), dict(eps=0.0), dict(pre="none"), dict(pad=8, off=8), dict(pad=1, off=3),
+                                dict(beta=0.0), dict(post="rms", wt=BF16, offset=1.0)])
+def test_step_options(kw):
+    for n, c in ((3, 320), (2, 1001), (4, 4096), (1, 17000)):
+        _step(np.random.default_rng(2), n, c, BF16, **kw)
+
+
+def test_step_rows_without_spread_and_not_finite():
+    a = api()
+    c = 512
+    x = torch.zeros(6, c, dtype=BF16, device="cuda")
+    r = torch.zeros(6, c, dtype=BF16, device="cuda")
+    r[1] = 3.0                       # a layer norm of equal values is zero
+    r[2, 5] = float("nan")
+    r[3, 7] = float("inf")
+    r[4] = torch.randn(c, device="cuda").to(BF16)
+    q, s, y = torch.full((6, c), 9, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda"), torch.empty(6, c, dtype=BF16, device="cuda")
+    a.f8_norm_quantize(x, q, s, y, residual=r, pre_norm=a.F8_NORM_LAYER)
+    for i in (0, 1, 5):
+        assert float(s[i]) == 0 and not q[i].any() and not y[i].any()
+    for i in (2, 3):
+        assert torch.isnan(s[i]) and not q[i].any() and torch.isnan(y[i]).all()
+    assert float(s[4]) > 0 and int(q[4].abs().max()) == 127
+
+
+def test_rows_captured_and_replayed():
+    a = api()
+    n, c = 65, 2048
+    x, r = torch.randn(n, c, device="cuda").to(BF16), torch.randn(n, c, device="cuda").to(BF16)
+    w = torch.ones(c, device="cuda")
+    q, s, so = torch.empty(n, c, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(r)
+    q2, s2 = torch.empty_like(q), torch.empty_like(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        a.f8_norm_quantize(x, q, s, residual=r, residual_out=so, pre_w=w)
+        a.f8_quantize_rows(so, q2, s2)
+    x.copy_(torch.randn(n, c, device="cuda"))
+    g.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (q, s, so, q2, s2)]
+    a.f8_norm_quantize(x, q, s, residual=r, residual_out=so, pre_w=w)
+    a.f8_quantize_rows(so, q2, s2)
+    assert all(torch.equal(u, v) for u, v in zip(got, (q, s, so, q2, s2)))
+    same_codes(so.float(), q2, s2)
+
+
+def test_no_rows():
+    a = api()
+    x = torch.zeros(0, 64, device="cuda")
+    a.f8_quantize_rows(x, torch.zeros(0, 64, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda"))
+    a.f8_norm_quantize(x, torch.zeros(0, 64, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda"))
