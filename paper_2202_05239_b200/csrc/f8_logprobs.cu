@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LpParams p) {
         if (e > 0.f) t += e * d;
     }
     r = block_reduce<LP_THREADS>(r, SumOp(), froom);
+    __syncthreads();
     t = block_reduce<LP_THREADS>(t, SumOp(), froom);
     const float lse = log1pf(r);
     auto logprob = [&](uint32_t o) { return bad ? __int_as_float(0x7fffffff) : empty ? -INFINITY : -Logit<T>::distance(top, o, p.c) - lse; };
@@ -93,6 +94,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(LpParams p) {
             const unsigned long long k = key(j);
             if (k < best) next = max(next, k);
         }
+        __syncthreads();
         best = block_reduce<LP_THREADS>(next, MaxOp(), room);
     }
 }

@@ -1,0 +1,455 @@
+// What lies between two blocks of a transformer, in one pass over its rows (f8_norm_quantize):
+//
+//     t = r + beta * g(gate) * post(x);   v = pre(t);   a = max |v|;  s = a / 127;  i = 127 / a;  q = floor(v * i + 1/2)
+//
+// Bound by memory traffic: x, r (and a gate per token) are read once, t, q and the values written once; what a row needs besides is two to
+// five sums over it.  Rows of up to 16384 elements stay in registers, a warp to 32 warps a row, while the next row is on its way.  A
+// block walks many rows, and up to 8192 elements each thread keeps the factors of its 8 elements (norm weights, the post norm's already
+// multiplied by beta and a gate that all rows share).  4096 x 8192 bf16, norms on both sides, channel gate: 68 us; with 32 elements a
+// thread and the weights read again for every row 73 us (half of them came from the second-level cache), with 16 elements, several
+// rows a block and the factors in shared memory 72 us.
+// Longer rows take a kernel that reads the row again for every sum, from the caches.
+#include "f8_rowdeal.cuh"
+
+namespace {
+
+struct NormParams {
+    int c, post_norm, pre_norm, gate_act;
+    float eps, weight_offset, branch_scale;
+    long long ldx, ldg, ldr, lds, ldy, ldq;
+    const void *x, *gate, *res, *post_w, *post_b, *pre_w, *pre_b;
+    void *sum;
+    int8_t *q;
+    float *scale;
+    void *y;
+};
+
+__device__ __forceinline__ float gate_value(float g, int act) {
+    return act == F8_ACT_SIGMOID ? activate<F8_ACT_SIGMOID>(g) : act == F8_ACT_TANH ? activate<F8_ACT_TANH>(g) : g;
+}
+
+// z -> (z - mean) * rstd * (w + offset) + b
+template <typename W>
+struct Norm {
+    const W *w, *b;
+    float mean, rstd, offset;
+    bool on;
+    __device__ __forceinline__ float operator()(float z, int i) const {
+        if (!on) return z;
+        z = (z - mean) * rstd;
+        if (w) z *= to_float(w[i]) + offset;
+        if (b) z += to_float(b[i]);
+        return z;
+    }
+};
+
+template <typename T, typename W>
+__global__ void __launch_bounds__(ROW_THREADS) long_norm_kernel(NormParams p) {
+    wait_for_stream();
+    let_stream_go_on();
+    __shared__ float room[4][32];
+    __shared__ uint32_t uroom[32];
+    const long long row = blockIdx.x;
+    const T *x = (const T *)p.x + row * p.ldx, *g = p.gate ? (const T *)p.gate + row * p.ldg : nullptr;
+    const T *r = p.res ? (const T *)p.res + row * p.ldr : nullptr;
+    T *sum = p.sum ? (T *)p.sum + row * p.lds : nullptr, *y = p.y ? (T *)p.y + row * p.ldy : nullptr;
+    int8_t *q = p.q ? p.q + row * p.ldq : nullptr;
+    // mean and 1 / deviation of what `f` gives over the row (the deviation from the mean: a second pass)
+    auto measure = [&](int kind, auto f, float &mean, float &rstd, float (*room)[32]) {
+        mean = 0.f;
+        rstd = 1.f;
+        if (kind == F8_NORM_NONE) return;
+        if (kind == F8_NORM_LAYER) {
+            float s = 0.f;
+            for (int i = threadIdx.x; i < p.c; i += ROW_THREADS) s += f(i);
+            mean = block_reduce<ROW_THREADS>(s, SumOp(), room[0]) / (float)p.c;
+        }
+        float s = 0.f;
+        for (int i = threadIdx.x; i < p.c; i += ROW_THREADS) {
+            const float z = f(i) - mean;
+            s += z * z;
+        }
+        rstd = 1.f / sqrtf(block_reduce<ROW_THREADS>(s, SumOp(), room[1]) / (float)p.c + p.eps);
+    };
+    Norm<W> post = {(const W *)p.post_w, (const W *)p.post_b, 0.f, 1.f, p.weight_offset, p.post_norm != F8_NORM_NONE};
+    Norm<W> pre = {(const W *)p.pre_w, (const W *)p.pre_b, 0.f, 1.f, p.weight_offset, p.pre_norm != F8_NORM_NONE};
+    measure(p.post_norm, [&](int i) { return to_float(x[i]); }, post.mean, post.rstd, room);
+    auto total = [&](int i) {
+        float z = post(to_float(x[i]), i);
+        if (g) z *= gate_value(to_float(g[i]), p.gate_act);
+        return fmaf(p.branch_scale, z, r ? to_float(r[i]) : 0.f);
+    };
+    measure(p.pre_norm, total, pre.mean, pre.rstd, room + 2);
+    RowScale s(0);
+    if (q) {
+        uint32_t peak = 0;
+        for (int i = threadIdx.x; i < p.c; i += ROW_THREADS) peak = max(peak, magnitude(pre(total(i), i)));
+        s = RowScale(block_reduce<ROW_THREADS>(peak, UMaxOp(), uroom));
+        if (threadIdx.x == 0) p.scale[row] = s.scale;
+    }
+    for (int i = threadIdx.x; i < p.c; i += ROW_THREADS) {
+        const float t = total(i), v = pre(t, i);
+        if (sum) sum[i] = from_float<T>(t);
+        if (q) {
+            const int code = s.code(v);
+            q[i] = (int8_t)code;
+            if (y) y[i] = from_float<T>((float)code * s.scale);
+        } else if (y) {
+            y[i] = from_float<T>(v);
+        }
+    }
+}
+
+
+// One value of the threads of a row.  Every warp writes its part to its own word of `room`, which no other reduction uses within two barriers.
+template <int THREADS, typename V, typename Op>
+__device__ __forceinline__ V row_gather(Op op, const V *room) {
+    constexpr int WARPS = THREADS / 32;
+    V v = room[threadIdx.x & (WARPS - 1)];
+#pragma unroll
+    for (int d = WARPS / 2; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float *room) {
+    v = warp_reduce(v, SumOp());
+    if (THREADS == 32) return v;
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return row_gather<THREADS>(SumOp(), room);
+}
+
+template <typename T, RowMode MODE, int THREADS, int E>
+__global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_norm_kernel(NormParams p, bool w32, long long n) {
+    wait_for_stream();
+    let_stream_go_on();
+    constexpr int BLOCK = row_block(THREADS), GROUPS = BLOCK / THREADS;
+    extern __shared__ uint4 smem[];
+    __shared__ float rooms[2][4][32];
+    __shared__ uint32_t urooms[2][32];
+    using D = Deal<T, MODE, THREADS, E>;
+    constexpr int PER = D::PER, PAIRS = D::PAIRS;
+    constexpr bool PIPE = MODE != LOOSE, KEEP = E == 8 && MODE != SHIFT;      // (shifted rows meet other weights from row to row)
+    const float per = 1.f / (float)p.c;
+    const bool own_gate = p.gate && p.ldg, fold = !p.post_b;
+    const int tensors = 1 + (p.res ? 1 : 0) + (own_gate ? 1 : 0), gate_at = tensors - 1;
+    const Ring<BLOCK, PER> ring(smem, tensors);
+    const long long step = (long long)gridDim.x * GROUPS;
+    long long row = GROUPS == 1 ? blockIdx.x : (long long)(threadIdx.x / THREADS) * gridDim.x + blockIdx.x;
+    const T *nx = (const T *)p.x + row * p.ldx, *nr = (const T *)p.res + row * p.ldr, *ng = (const T *)p.gate + row * p.ldg;    // rows on their way
+    auto send = [&](bool some, int stage) {
+        if (some) {
+            const D d(nx, p.c);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                d.send(nx, j, ring.place(stage, 0, j));
+                if (p.res) d.send(nr, j, ring.place(stage, 1, j));
+                if (own_gate) d.send(ng, j, ring.place(stage, gate_at, j));
+            }
+        }
+        ring_commit();
+        nx += step * p.ldx;
+        nr += step * p.ldr;
+        ng += step * p.ldg;
+    };
+    const T *cx = nx, *cr = nr, *cg = ng;          // the row at work
+    if (PIPE) send(row < n, 0);
+    auto weight = [&](const void *w, int i) { return w ? (sizeof(T) == 4 || w32 ? ((const float *)w)[i] : to_float(((const T *)w)[i])) + p.weight_offset : 1.f; };
+    // the factor of x / deviation in the residual sum: weight, beta and a shared gate (with a bias behind the post norm the weight alone)
+    auto post_weight = [&](int i) {
+        float f = weight(p.post_w, i);
+        if (!fold) return f;
+        f *= p.branch_scale;
+        return p.gate && !own_gate ? f * gate_value(to_float(((const T *)p.gate)[i]), p.gate_act) : f;
+    };
+    auto factor = [&](const D &d, int j, F2 (&f)[PAIRS], bool post) {
+        float e[D::VEC];
+#pragma unroll
+        for (int k = 0; k < D::VEC; ++k) {
+            const int i = d.at(j, k);
+            e[k] = !d.in(j, k) ? 0.f : post ? post_weight(i) : weight(p.pre_w, i);
+        }
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) f[i] = pair(e[2 * i], e[2 * i + 1]);
+    };
+    F2 kept[KEEP ? 2 : 1][PER][PAIRS];
+    if (KEEP) {
+        const D d((const T *)p.x, p.c);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            factor(d, j, kept[0][j], true);
+            factor(d, j, kept[KEEP ? 1 : 0][j], false);
+        }
+    }
+    auto activate_gate = [&](F2 (&f)[PAIRS]) {
+        if (p.gate_act == F8_ACT_NONE) return;
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            const float2 g = halves(f[i]);
+            f[i] = pair(gate_value(g.x, p.gate_act), gate_value(g.y, p.gate_act));
+        }
+    };
+    T *sum = (T *)p.sum + row * p.lds, *y = (T *)p.y + row * p.ldy;
+    int8_t *q = p.q + row * p.ldq;
+    for (int stage = 0; row < n; row += step, stage ^= 1) {
+        float (*const room)[32] = rooms[stage];
+        uint32_t *const uroom = urooms[stage];
+        const D d(cx, p.c);
+        if (PIPE) {
+            send(row + step < n, stage ^ 1);
+            ring_wait();
+        }
+        F2 v[PER][PAIRS];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(cx, j), v[j]);
+        // v <- (v - mean) / deviation
+        auto standardize = [&](int kind, float (*rm)[32]) {
+            F2 s = 0ull;
+            if (kind == F8_NORM_LAYER) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) s = add2(s, v[j][i]);
+                const float2 h = halves(s);
+                const F2 mean = both(-row_sum<THREADS>(h.x + h.y, rm[0]) * per);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[j][i] = add2(v[j][i], mean);
+                    d.mask(j, v[j]);
+                }
+                s = 0ull;
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) s = fma2(v[j][i], v[j][i], s);
+            const float2 h = halves(s);
+            const F2 rstd = both(rsqrtf(row_sum<THREADS>(h.x + h.y, rm[1]) * per + p.eps));
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], rstd);
+        };
+        auto by_factors = [&](bool post) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                F2 f[PAIRS];
+                if (!KEEP) factor(d, j, f, post);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], KEEP ? kept[KEEP && !post ? 1 : 0][j][i] : f[i]);
+            }
+        };
+        auto plus = [&](const void *b) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                if (!d.on(j)) continue;
+                F2 f[PAIRS];
+                if (sizeof(T) == 4 || w32) d.template weights<true>(b, j, f);
+                else d.template weights<sizeof(T) == 4>(b, j, f);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = add2(v[j][i], f[i]);
+            }
+        };
+        if (p.post_norm != F8_NORM_NONE) standardize(p.post_norm, room);
+        if (!fold) {
+            by_factors(true);
+            plus(p.post_b);
+            if (p.gate && !own_gate) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (!d.on(j)) continue;
+                    F2 f[PAIRS];
+                    d.template weights<sizeof(T) == 4>(p.gate, j, f);
+                    activate_gate(f);
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
+                }
+            }
+        }
+        if (own_gate) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                F2 f[PAIRS];
+                unpack<T>(PIPE ? d.take(j, ring.place(stage, gate_at, j)) : d.load(cg, j), f);
+                activate_gate(f);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
+            }
+        }
+        // the residual sum
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            F2 f[PAIRS], t[PAIRS];
+            if (fold && KEEP) {
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) f[i] = kept[0][j][i];
+            } else if (fold) {
+                factor(d, j, f, true);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) f[i] = both(p.branch_scale);
+            }
+            if (p.res) {
+                unpack<T>(PIPE ? d.take(j, ring.place(stage, 1, j)) : d.load(cr, j), t);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = fma2(v[j][i], f[i], t[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
+            }
+            if (p.sum) d.store(sum, j, v[j]);
+        }
+        T *const my_y = y;
+        int8_t *const my_q = q;
+        cx += step * p.ldx;
+        cr += step * p.ldr;
+        cg += step * p.ldg;
+        sum += step * p.lds;
+        y += step * p.ldy;
+        q += step * p.ldq;
+        if (!p.q && !p.y) continue;
+        float peak = 0.f;
+        uint32_t top;
+        if (p.q && p.pre_norm == F8_NORM_RMS && !p.pre_b) {
+            // the sum of squares and max |t w| in one reduction: v = (t w) * rstd, and the product with one rstd keeps the order
+            F2 s = 0ull;
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) s = fma2(v[j][i], v[j][i], s);
+            by_factors(false);
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) peak = peak_of(peak, v[j][i]);
+            const float2 h = halves(s);
+            float sq = warp_reduce(h.x + h.y, SumOp());
+            top = warp_reduce(magnitude(peak), UMaxOp());
+            if (THREADS != 32) {
+                if ((threadIdx.x & 31) == 0) {
+                    room[2][threadIdx.x >> 5] = sq;
+                    uroom[threadIdx.x >> 5] = top;
+                }
+                __syncthreads();
+                sq = row_gather<THREADS>(SumOp(), room[2]);
+                top = row_gather<THREADS>(UMaxOp(), uroom);
+            }
+            const float rstd = rsqrtf(sq * per + p.eps);
+            top = magnitude(__uint_as_float(top) * rstd);
+            const F2 f = both(rstd);
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f);
+        } else {
+            if (p.pre_norm != F8_NORM_NONE) {
+                standardize(p.pre_norm, room + 2);
+                by_factors(false);
+                if (p.pre_b) plus(p.pre_b);
+            }
+            if (!p.q) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) d.store(my_y, j, v[j]);
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) peak = peak_of(peak, v[j][i]);
+            top = warp_reduce(magnitude(peak), UMaxOp());
+            if (THREADS != 32) {
+                if ((threadIdx.x & 31) == 0) uroom[threadIdx.x >> 5] = top;
+                __syncthreads();
+                top = row_gather<THREADS>(UMaxOp(), uroom);
+            }
+        }
+        const RowScale s = RowScale::of_warp(top);
+        if (threadIdx.x % THREADS == 0) p.scale[row] = s.scale;
+        emit<T>(d, v, s, top < 0x7f800000u, my_q, p.y ? my_y : nullptr);
+    }
+}
+
+template <typename T, RowMode MODE, int THREADS, int E>
+cudaError_t launch_row_norm_at(const NormParams &p, bool w32, long long n, cudaStream_t st) {
+    constexpr int PER = E * (int)sizeof(T) / 16;
+    const int tensors = 1 + (p.res ? 1 : 0) + (p.gate && p.ldg ? 1 : 0);
+    if (MODE != LOOSE && ring_bytes(THREADS, PER, tensors) <= RING_MOST)
+        return launch_ring<row_norm_kernel<T, MODE, THREADS, E>>(THREADS, PER, tensors, n, st, p, w32);
+    return launch_ring<row_norm_kernel<T, LOOSE, THREADS, E>>(THREADS, PER, 0, n, st, p, w32);
+}
+template <typename T, RowMode MODE>
+cudaError_t launch_row_norm(const NormParams &p, bool w32, long long n, cudaStream_t st) {
+    const int need = p.c + (MODE == SHIFT ? 16 / (int)sizeof(T) - 1 : 0);
+    if (need <= 32 * 8) return launch_row_norm_at<T, MODE, 32, 8>(p, w32, n, st);
+    if (need <= 128 * 8) return launch_row_norm_at<T, MODE, 128, 8>(p, w32, n, st);
+    if (need <= 256 * 8) return launch_row_norm_at<T, MODE, 256, 8>(p, w32, n, st);
+    if (need <= 512 * 8) return launch_row_norm_at<T, MODE, 512, 8>(p, w32, n, st);
+    if (need <= 1024 * 8) return launch_row_norm_at<T, MODE, 1024, 8>(p, w32, n, st);
+    return launch_row_norm_at<T, MODE, 1024, 16>(p, w32, n, st);
+}
+
+template <typename T>
+cudaError_t launch_norm(const NormParams &p, long long n, bool w32, cudaStream_t st) {
+    constexpr int VEC = 16 / sizeof(T);
+    RowLayout l(n, sizeof(T), p.c);
+    l.add(p.x, p.ldx, sizeof(T));
+    l.add(p.res, p.ldr, sizeof(T));
+    l.add(p.sum, p.lds, sizeof(T));
+    l.add(p.y, p.ldy, sizeof(T));
+    l.add(p.q, p.ldq, 1);
+    if (p.gate && p.ldg) l.add(p.gate, p.ldg, sizeof(T));
+    if (p.gate && !p.ldg) l.vector(p.gate);
+    l.vector(p.post_w);
+    l.vector(p.post_b);
+    l.vector(p.pre_w);
+    l.vector(p.pre_b);
+    if (l.same && !l.shift() && p.c <= ROW_MOST) return launch_row_norm<T, PLAIN>(p, w32, n, st);
+    if (l.same && p.c + VEC - 1 <= ROW_MOST) return launch_row_norm<T, SHIFT>(p, w32, n, st);
+    if (p.c <= ROW_MOST) return launch_row_norm<T, LOOSE>(p, w32, n, st);
+    const dim3 grid((unsigned)n);
+    if (w32) return launch_early(long_norm_kernel<T, float>, grid, ROW_THREADS, 0, st, p);
+    return launch_early(long_norm_kernel<T, T>, grid, ROW_THREADS, 0, st, p);
+}
+
+}   // namespace
+
+extern "C" f8_status f8_norm_quantize(const f8_norm_desc *desc, const void *x, const void *gate, const void *residual, const void *post_w,
+                           const void *post_b, const void *pre_w, const void *pre_b, void *residual_out, int8_t *q, float *scale,
+                           void *y, void *cuda_stream) {
+    if (!desc) return f8_set_error(F8_ERR_NULL, "descriptor is NULL");
+    f8_norm_desc d = *desc;
+    if (d.n < 0 || d.n > 0x7fffffffll || d.c <= 0) return f8_set_error(F8_ERR_SHAPE, "n in 0 .. 2^31 - 1 and c > 0 are needed");
+    const int size = real_size(d.dtype);
+    if (!size) return f8_set_error(F8_ERR_DTYPE, "dtype must be F8_F32, F8_F16 or F8_BF16");
+    if (d.w_dtype != F8_F32 && d.w_dtype != d.dtype) return f8_set_error(F8_ERR_DTYPE, "w_dtype must be F8_F32 or dtype");
+    if (d.post_norm < F8_NORM_NONE || d.post_norm > F8_NORM_LAYER || d.pre_norm < F8_NORM_NONE || d.pre_norm > F8_NORM_LAYER)
+        return f8_set_error(F8_ERR_UNSUPPORTED, "a norm must be F8_NORM_NONE, F8_NORM_RMS or F8_NORM_LAYER");
+    if (d.gate_act != F8_ACT_NONE && d.gate_act != F8_ACT_SIGMOID && d.gate_act != F8_ACT_TANH)
+        return f8_set_error(F8_ERR_UNSUPPORTED, "gate_act must be F8_ACT_NONE, F8_ACT_SIGMOID or F8_ACT_TANH");
+    if ((d.post_norm == F8_NORM_NONE && (post_w || post_b)) || (d.pre_norm == F8_NORM_NONE && (pre_w || pre_b)))
+        return f8_set_error(F8_ERR_UNSUPPORTED, "weights of a norm that is F8_NORM_NONE");
+    if (!(d.eps >= 0.f) || !isfinite(d.eps) || !isfinite(d.weight_offset) || !isfinite(d.branch_scale))
+        return f8_set_error(F8_ERR_SHAPE, "eps must be finite and not negative, weight_offset and branch_scale finite");
+    if (gate && d.gate_rows != 1 && d.gate_rows != d.n) return f8_set_error(F8_ERR_SHAPE, "gate_rows must be 1 or n");
+    if (!row_distance(&d.ldx, d.c, d.n) || !row_distance(&d.ldg, d.c, d.n) || !row_distance(&d.ldr, d.c, d.n) || !row_distance(&d.lds, d.c, d.n) ||
+        !row_distance(&d.ldy, d.c, d.n) || !row_distance(&d.ldq, d.c, d.n))
+        return f8_set_error(F8_ERR_SHAPE, "a row distance is smaller than the row, or too large");
+    if (d.n == 0) return F8_OK;
+    if (!x || (!q && !y && !residual_out) || (q && !scale) || (!q && scale))
+        return f8_set_error(F8_ERR_NULL, "x, and an output (q with scale, y or residual_out), must not be NULL");
+    const int ws = real_size(d.w_dtype);
+    if (misaligned(x, size) || misaligned(gate, size) || misaligned(residual, size) || misaligned(residual_out, size) || misaligned(y, size) ||
+        misaligned(post_w, ws) || misaligned(post_b, ws) || misaligned(pre_w, ws) || misaligned(pre_b, ws) || misaligned(scale, 4))
+        return f8_set_error(F8_ERR_ALIGN, "a pointer is not aligned to its element");
+    if (f8_pending_timeout() != F8_OK) return F8_ERR_TIMEOUT;
+    NormParams p = {d.c, d.post_norm, d.pre_norm, d.gate_act, d.eps, d.weight_offset, d.branch_scale, d.ldx, d.gate_rows == 1 ? 0 : d.ldg,
+                    d.ldr, d.lds, d.ldy, d.ldq, x, gate, residual, post_w, post_b, pre_w, pre_b, residual_out, q, scale, y};
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    const bool w32 = d.w_dtype == F8_F32;
+    const cudaError_t e = d.dtype == F8_F32   ? launch_norm<float>(p, d.n, true, st)
+                          : d.dtype == F8_F16 ? launch_norm<__half>(p, d.n, w32, st)
+                                              : launch_norm<__nv_bfloat16>(p, d.n, w32, st);
+    if (e != cudaSuccess) return f8_set_error(F8_ERR_CUDA, cudaGetErrorString(e));
+    return F8_OK;
+}

@@ -20,19 +20,31 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 struct SumOp { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct UMaxOp { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; } };
 
-// One value of the whole block, the same in every thread and in every run (fixed order).  `room`: 32 words of shared memory.
-template <int THREADS, typename V, typename Op>
-__device__ __forceinline__ V block_reduce(V v, Op op, V *room) {
+// One value of a whole warp / block, the same in every thread and in every run (fixed order).  `room`: 32 words of shared memory that
+// no other reduction of the kernel uses within two barriers.
+__device__ __forceinline__ uint32_t warp_reduce(uint32_t v, UMaxOp) { return __reduce_max_sync(0xffffffffu, v); }
+template <typename V, typename Op>
+__device__ __forceinline__ V warp_reduce(V v, Op op) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+template <int THREADS, typename V, typename Op>
+__device__ __forceinline__ V block_reduce(V v, Op op, V *room) {
+    v = warp_reduce(v, op);
     if (THREADS == 32) return v;
     constexpr int WARPS = THREADS / 32;
-    __syncthreads();                        // the room may still be read from the reduction before
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = room[0];
+    if (WARPS <= 8) {
+        v = room[0];
 #pragma unroll
-    for (int w = 1; w < WARPS; ++w) v = op(v, room[w]);
+        for (int w = 1; w < WARPS; ++w) v = op(v, room[w]);
+    } else {
+        v = room[threadIdx.x & (WARPS - 1)];
+#pragma unroll
+        for (int d = WARPS / 2; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
+    }
     return v;
 }
 
@@ -49,6 +61,19 @@ struct RowScale {
         scale = zeros ? 0.f : __fdiv_rn(a, 127.f);
         inverse = zeros || !finite ? 0.f : __fdiv_rn(127.f, a);
     }
+    // The same for a whole warp that holds one peak: one division, by the even lanes of the first quotient, by the odd ones of the second.
+    static __device__ __forceinline__ RowScale of_warp(uint32_t peak) {
+        const float a = __uint_as_float(peak);
+        const bool odd = threadIdx.x & 1;
+        const float q = __fdiv_rn(odd ? 127.f : a, odd ? a : 127.f);
+        RowScale s;
+        s.scale = __shfl_sync(0xffffffffu, q, 0);
+        s.inverse = __shfl_sync(0xffffffffu, q, 1);
+        if (a < 0x1p-100f) s.scale = 0.f;
+        if (a < 0x1p-100f || peak >= 0x7f800000u) s.inverse = 0.f;
+        return s;
+    }
+    __device__ __forceinline__ RowScale() {}
     // floor(v * inverse + 1/2): the sum is rounded towards -infinity, which no integer lies under, so the floor is that of the exact
     // sum.  |v * inverse| <= 127 (1 + 2^-23), hence |code| <= 127 without a clip.  NaN (from 0 * infinity) converts to 0.
     __device__ __forceinline__ int code(float v) const { return __float2int_rd(__fmaf_rd(v, inverse, 0.5f)); }
