@@ -25,7 +25,11 @@
 namespace {
 
 constexpr int LP_THREADS = 256;
-constexpr int LP_UNROLL = 4;              // vectors of 16 bytes a thread has on their way
+// Vectors of 16 bytes a thread takes at once, and blocks an SM has room for (64 registers a thread).  What overlaps loads with arithmetic
+// here is other blocks: 1024 x 50001 float, entropy: 4 and 4 38 us; 8 and 3 42; 4, the next 4 ahead in registers, and 3 43; three
+// stages of 4 through shared memory and 3 40; 2 and 6 51; 4 and 5 41.
+constexpr int LP_UNROLL = 4;
+constexpr int LP_BLOCKS = 4;
 constexpr int LP_CANDIDATES = 1024;       // rows with more (as when one thread's elements hold most of the large ones) take the slow way
 constexpr int LP_MOST_TOP = 32;
 
@@ -65,6 +69,7 @@ template <typename T> struct Num {
     static __device__ __forceinline__ V larger(V a, V b) { return fmaxf(a, b); }
     static __device__ __forceinline__ V safe(V m) { return m == -INFINITY ? 0.f : m; }      // a reference to subtract: -infinity - -infinity is NaN
     static __device__ __forceinline__ float minus(V x, V m) { return x - m; }
+    static __device__ __forceinline__ F2 minus2(V x, V y, V m) { return add2(pair(x, y), both(-m)); }
     static __device__ __forceinline__ V one(const T *p) { return to_float(*p); }
     static __device__ __forceinline__ void unpack(const uint4 &w, V (&x)[VEC]) {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -94,29 +99,41 @@ template <> struct Num<int> {
     static __device__ __forceinline__ V larger(V a, V b) { return max(a, b); }
     static __device__ __forceinline__ V safe(V m) { return m; }
     static __device__ __forceinline__ float minus(V x, V m) { return -(float)((uint32_t)m - (uint32_t)x); }       // m >= x
+    static __device__ __forceinline__ F2 minus2(V x, V y, V m) { return pair(minus(x, m), minus(y, m)); }
     static __device__ __forceinline__ V one(const int *p) { return *p; }
     static __device__ __forceinline__ void unpack(const uint4 &w, V (&x)[4]) { x[0] = (int)w.x; x[1] = (int)w.y; x[2] = (int)w.z; x[3] = (int)w.w; }
     static __device__ __forceinline__ bool bad(uint32_t) { return false; }
     static __device__ __forceinline__ bool empty(uint32_t) { return false; }
 };
 
-// Sums over some of the elements x relative to m: s of exp((x - m) c), t of (x - m) exp((x - m) c).
+// Sums over some of the elements x relative to m: s of exp((x - m) c), t of (x - m) exp((x - m) c), each in two halves.
 template <typename T>
 struct Sums {
-    typename Num<T>::V m;
-    float s, t;
-    __device__ __forceinline__ void add(typename Num<T>::V x, typename Num<T>::V ref, float cl) {
+    typedef typename Num<T>::V V;
+    V m;
+    F2 s, t;
+    // two more elements, at most m
+    __device__ __forceinline__ void add(V x, V y, V ref, float cl) {
+        const F2 d = Num<T>::minus2(x, y, ref);
+        const float2 z = halves(mul2(d, both(cl))), f = halves(d);
+        const F2 e = pair(exp2_fast(z.x), exp2_fast(z.y));
+        s = add2(s, e);
+        t = fma2(e, pair(fmaxf(f.x, -3e38f), fmaxf(f.y, -3e38f)), t);       // (0 * infinity)
+    }
+    __device__ __forceinline__ void add(V x, V ref, float cl) {
         const float d = Num<T>::minus(x, ref), e = exp2_fast(d * cl);
-        s += e;
-        t = fmaf(e, fmaxf(d, -3e38f), t);       // (0 * infinity)
+        s = add2(s, pair(e, 0.f));
+        t = fma2(pair(e, 0.f), pair(fmaxf(d, -3e38f), 0.f), t);
     }
     // the sums relative to a larger m (which is none of the elements met so far)
-    __device__ __forceinline__ void raise(typename Num<T>::V to, float cl) {
+    __device__ __forceinline__ void raise(V to, float cl) {
         const float d = fmaxf(Num<T>::minus(m, to), -3e38f), f = exp2_fast(d * cl);
-        t = f * fmaf(s, d, t);
-        s *= f;
+        t = mul2(both(f), fma2(s, both(d), t));
+        s = mul2(s, both(f));
         m = to;
     }
+    __device__ __forceinline__ float sum_s() const { const float2 f = halves(s); return f.x + f.y; }
+    __device__ __forceinline__ float sum_t() const { const float2 f = halves(t); return f.x + f.y; }
 };
 
 // What a block has found of its part of the row: read by the leading block of the cluster.
@@ -126,6 +143,17 @@ struct LpPart {
     int too_many;                           // more candidates than there is room for
     Key top[LP_MOST_TOP];                   // the part's alternatives in falling order, 0 behind the last
 };
+
+// how many of n keys are larger
+__device__ __forceinline__ int above_in(const Key *keys, int n, Key k) {
+    int above = 0, j = 0;
+    for (; j + 8 <= n; j += 8) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) above += keys[j + u] > k ? 1 : 0;
+    }
+    for (; j < n; ++j) above += keys[j] > k ? 1 : 0;
+    return above;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ void cluster_sync() {
@@ -141,7 +169,7 @@ __device__ __forceinline__ Key remote64(uint32_t a) { Key v; asm volatile("ld.sh
 __device__ __forceinline__ uint32_t remote32(uint32_t a) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory"); return v; }
 
 template <typename T, bool CLUSTER>
-__global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
+__global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParams p) {
     wait_for_stream();
     let_stream_go_on();
     typedef Num<T> N;
@@ -170,7 +198,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
     // ---- one pass: a thread takes every 256th vector, the first threads an element of the head or the tail
     Sums<T> sum;
     sum.m = N::lowest();
-    sum.s = sum.t = 0.f;
+    sum.s = sum.t = 0ull;
     bool some = false;
     int at = 0, span = 0;                   // where the largest element lies: at .. at + span
     auto meet = [&](V x, int index) {
@@ -210,7 +238,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
         for (int u = 0; u < LP_UNROLL; ++u) {
             if (u >= count) break;
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) sum.add(x[u][k], ref, cl);
+            for (int k = 0; k < VEC; k += 2) sum.add(x[u][k], x[u][k + 1], ref, cl);
         }
     };
     auto vector = [&](int i) {
@@ -219,14 +247,13 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
         return w;
     };
     int i = tid;
+    uint4 w[LP_UNROLL];
     for (; i + (LP_UNROLL - 1) * LP_THREADS < vecs; i += LP_UNROLL * LP_THREADS) {
-        uint4 w[LP_UNROLL];
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u) w[u] = vector(i + u * LP_THREADS);
         batch(w, LP_UNROLL, i);
     }
     for (; i < vecs; i += LP_THREADS) {
-        uint4 w[LP_UNROLL];
         w[0] = vector(i);
         batch(w, 1, i);
     }
@@ -244,10 +271,11 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
         float s = 0.f, t = 0.f;
         if (some) {
             const float d = lost ? 0.f : fmaxf(N::minus(sum.m, m), -3e38f), f = exp2_fast(d * cl);
-            t = f * fmaf(sum.s, d, sum.t);
-            s = owner ? 0.f : f * sum.s;
-            if (f == 0.f && sum.s == sum.s) s = t = 0.f;
-            if (owner && sum.s != sum.s) s = sum.s;
+            const float own_s = sum.sum_s(), own_t = sum.sum_t();
+            t = f * fmaf(own_s, d, own_t);
+            s = owner ? 0.f : f * own_s;
+            if (f == 0.f && own_s == own_s) s = t = 0.f;
+            if (owner && own_s != own_s) s = own_s;
         }
         keys[tid] = high;
         __syncthreads();
@@ -300,19 +328,18 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) bound = max(bound, __shfl_xor_sync(0xffffffffu, bound, d));
         // ... and the top-th largest of their own maxima is the bound of the elements
-        if (low >= bound && low) found[atomicAdd(&counts[0], 1)] = low;
-        __syncthreads();
-        const int threads = counts[0];
-        if (tid < threads) {
-            const Key k = found[tid];
-            int n_above = 0;
-            for (int j = 0; j < threads; ++j) n_above += found[j] > k ? 1 : 0;
-            if (n_above == p.top - 1) room[1][0] = k;
+        Key least = bound;
+        const int rounds = (vecs + LP_THREADS - 1) / LP_THREADS;
+        if (rounds > 4) {           // (a thread with a handful of vectors is read again sooner than its worth is looked into)
+            if (low >= bound && low) found[atomicAdd(&counts[0], 1)] = low;
+            __syncthreads();
+            const int threads = counts[0];
+            if (tid < threads && above_in(found, threads, found[tid]) == p.top - 1) room[1][0] = found[tid];
+            __syncthreads();
+            least = threads >= p.top ? room[1][0] : 0;      // (fewer threads with elements than alternatives: all elements)
+            __syncthreads();
+            if (tid == 0) counts[0] = 0;
         }
-        __syncthreads();
-        const Key least = threads >= p.top ? room[1][0] : 0;      // (fewer threads with elements than alternatives: all elements)
-        __syncthreads();
-        if (tid == 0) counts[0] = 0;
         if (some && high >= least) members[atomicAdd(&counts[1], 1)] = tid;
         __syncthreads();
         auto offer = [&](V x, int index) {
@@ -321,7 +348,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
             const int n = atomicAdd(&counts[0], 1);
             if (n < LP_CANDIDATES) found[n] = k;
         };
-        const int who = counts[1], rounds = (vecs + LP_THREADS - 1) / LP_THREADS;
+        const int who = counts[1];
         for (int j = tid; j < who * rounds; j += LP_THREADS) {
             const int at_vec = (j / who) * LP_THREADS + members[j % who];
             if (at_vec >= vecs) continue;
@@ -339,10 +366,8 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
             if (tid == 0) part.too_many = 1;
         } else {
             for (int j = tid; j < n; j += LP_THREADS) {
-                const Key k = found[j];
-                int n_above = 0;
-                for (int q = 0; q < n; ++q) n_above += found[q] > k ? 1 : 0;
-                if (n_above < p.top) part.top[n_above] = k;
+                const int n_above = above_in(found, n, found[j]);
+                if (n_above < p.top) part.top[n_above] = found[j];
             }
         }
     }
@@ -383,8 +408,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
                 int n_above = LP_MOST_TOP;
                 if (tid < all) {
                     mine_top = found[tid];
-                    n_above = 0;
-                    for (int q = 0; q < all; ++q) n_above += found[q] > mine_top ? 1 : 0;
+                    n_above = above_in(found, all, mine_top);
                 }
                 __syncthreads();
                 if (mine_top && n_above < per) keys[n_above] = mine_top;
@@ -429,8 +453,8 @@ __global__ void __launch_bounds__(LP_THREADS, 4) logprobs_kernel(LpParams p) {
     if (CLUSTER) cluster_sync();            // no block goes while the leader may read it
 }
 
-// Blocks that share a row: enough of them to give every SM about two, as long as each has 16 KiB of the row.  16 rows of 131072 bf16:
-// one block a row LP_ONE us, eight LP_EIGHT us.
+// Blocks that share a row: enough of them to give every SM about two, as long as each has 16 KiB of the row.  16 rows of 131072 bf16,
+// 20 alternatives: one block a row 18.0 us, eight 12.6 us.
 int lp_blocks(long long n, long long row_bytes) {
     int s = 1;
     while (s < 8 && n * s < 296 && row_bytes / (2 * s) >= 16384) s *= 2;

@@ -34,16 +34,7 @@ __device__ __forceinline__ float activate(float v) {
 //   LOOSE   anything else: neighbouring threads take neighbouring elements one by one
 enum RowMode { PLAIN, SHIFT, LOOSE };
 
-// Two 32-bit floats in a register pair: this GPU adds and multiplies both in one instruction.  These kernels are bound by instruction
-// issue before they are by memory (norms on both sides, 4096 x 8192 bf16: 56 instructions an element took 81 us).
-typedef unsigned long long F2;
-__device__ __forceinline__ F2 pair(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float2 halves(F2 p) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p)); return r; }
-__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ F2 fma2_down(F2 a, F2 b, F2 c) { F2 r; asm("fma.rm.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
+// The row kernels are bound by instruction issue as much as by memory, so they work on pairs throughout.
 // the largest magnitude so far and two more; NaN wins
 __device__ __forceinline__ float peak_of(float m, F2 p) {
     const float2 f = halves(p);
