@@ -2,36 +2,16 @@
 //
 //     acc = sum_k x[i, k] w[j, k]   (exact, int32);     y[i, j] = round( fma((float)acc * sx[i], sw[j], b[j]) )
 //
-// The kernel here takes every extent, alignment and row distance: tiles of 64 x 64 on mma.sync m16n8k32, K in chunks of 64 bytes through
+// The tensor-core kernels (f8_scaled_tc.cu) fetch operands whose rows start at multiples of 16 bytes.  The kernel here takes every
+// alignment and row distance: tiles of 64 x 64 on mma.sync m16n8k32, K in chunks of 64 bytes through
 // padded rows of shared memory, the next chunk on its way in registers while one is multiplied.
 #include <math.h>
 
 #include <algorithm>
 
-#include "f8_real.cuh"
+#include "f8_scaled.h"
 
 namespace {
-
-struct ScaledParams {
-    int n, k, out;
-    int y_dtype, bias_dtype;
-    int x_scales, w_scales;
-    long long ldx, ldw, ldy;
-    const uint8_t *x, *w;
-    const float *xs, *ws;
-    const void *bias;
-    void *y;
-};
-
-__device__ __forceinline__ float load_real(const void *p, int dtype, long long i) {
-    return dtype == F8_F32 ? ((const float *)p)[i] : dtype == F8_F16 ? to_float(((const __half *)p)[i]) : to_float(((const __nv_bfloat16 *)p)[i]);
-}
-__device__ __forceinline__ void store_real(void *p, int dtype, long long i, float v) {
-    if (dtype == F8_F32) ((float *)p)[i] = v;
-    else if (dtype == F8_F16) ((__half *)p)[i] = from_float<__half>(v);
-    else ((__nv_bfloat16 *)p)[i] = from_float<__nv_bfloat16>(v);
-}
-__device__ __forceinline__ float scaled(int acc, float sx, float sw, float b) { return __fmaf_rn(__fmul_rn(__int2float_rn(acc), sx), sw, b); }
 
 // 16 bytes from `p`, those from `valid` on as zeros.  ALIGNED: p is a multiple of 16.  Otherwise the one or two 16-byte granules that
 // hold wanted bytes are read whole and shifted together; a granule that holds one byte of an allocation lies within its page.
@@ -207,7 +187,9 @@ extern "C" f8_status f8_linear_scaled(const f8_scaled_desc *desc, const void *x,
     if (f8_pending_timeout() != F8_OK) return F8_ERR_TIMEOUT;
     const ScaledParams p = {d.n, d.k, d.out, d.y_dtype, d.bias_dtype, d.x_scales, d.w_scales, d.ldx, d.ldw, d.ldy, (const uint8_t *)x,
                             (const uint8_t *)w, x_scale, w_scale, bias, y};
-    const cudaError_t e = launch_any(p, d.x_dtype == F8_S8, (cudaStream_t)cuda_stream);
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e = f8_force_direct() ? cudaErrorNotSupported : f8_scaled_tc_launch(p, d.x_dtype == F8_S8, f8_status_word(), st);
+    if (e == cudaErrorNotSupported) e = launch_any(p, d.x_dtype == F8_S8, st);
     if (e != cudaSuccess) return f8_set_error(F8_ERR_CUDA, cudaGetErrorString(e));
     return F8_OK;
 }
