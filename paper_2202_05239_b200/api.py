@@ -2,13 +2,13 @@
 
 Only argument marshalling happens here: every function forwards device pointers
 of torch tensors (torch supplies memory and streams) to the entry point of the
-same name in ``include/f8net.h``.  There is no CPU fallback: importing this
+same name in ``include/f8net.h`` (those on real-valued tensors through a C++
+module of this package, ``csrc/f8_torch.cpp``).  There is no CPU fallback: importing this
 module fails if the library has not been built.
 """
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from typing import Optional, Sequence
 
@@ -20,12 +20,14 @@ from . import synth
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libf8net.so")
 
-if not os.path.exists(_LIB_PATH):
+if not os.path.exists(_LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_f8torch.so")):
     raise ImportError(
-        f"{_LIB_PATH} is missing: build the CUDA library first "
+        f"{_LIB_PATH} or _f8torch.so is missing: build the CUDA library first "
         "(python -m paper_2202_05239_b200.build, or __graft_entry__.build())")
 
 _lib = ctypes.CDLL(_LIB_PATH)
+
+from . import _f8torch  # noqa: E402  (built beside the library; needs it and torch loaded)
 
 F8_OK = 0
 F8_U8, F8_S8, F8_S32, F8_S32_RELU = 0, 1, 2, 3
@@ -252,53 +254,7 @@ _lib.f8_quantize_rows.argtypes = [_vp] * 7
 _lib.f8_norm_quantize.argtypes = [_vp] * 13
 _lib.f8_token_logprobs.argtypes = [_vp] * 8
 
-_CODES = {torch.uint8: F8_U8, torch.int8: F8_S8, torch.int32: F8_S32, torch.float32: F8_F32, torch.float16: F8_F16, torch.bfloat16: F8_BF16}
-_REAL = (torch.float32, torch.float16, torch.bfloat16)
-
-
-def _bad(what: str):
-    raise ValueError(what)
-
-
-def _matrix(t: torch.Tensor, what: str, shape=None, dtypes=None, device: int = -1):
-    """(pointer, row distance) of a matrix with unit stride along its rows, checked against a shape, its types and a device."""
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
-        _bad(f"{what}: a matrix{' of shape ' + str(tuple(shape)) if shape is not None else ''} is needed, got {tuple(t.shape)}")
-    if dtypes is not None and t.dtype not in dtypes:
-        _bad(f"{what}: type {t.dtype} where one of {dtypes} is needed")
-    if t.get_device() < 0 or (device >= 0 and t.get_device() != device):
-        _bad(f"{what}: on {t.device}, not on the current CUDA device")
-    rows, cols = t.shape
-    step, unit = t.stride()
-    if rows > 0x7fffffff or cols > 0x7fffffff:
-        _bad(f"{what}: extents beyond 2^31 - 1")
-    if (unit != 1 and cols > 1) or (step < cols and rows > 1):
-        _bad(f"{what}: rows with unit stride that do not overlap are needed, got strides {t.stride()}")
-    return t.data_ptr(), step if rows > 1 else max(step, cols)
-
-
-def _vector(t: Optional[torch.Tensor], what: str, sizes, dtypes, device: int):
-    """Pointer of a dense vector (any shape with that many elements)."""
-    if t is None:
-        return None
-    if t.numel() not in sizes or t.dtype not in dtypes:
-        _bad(f"{what}: {sizes} elements of one of {dtypes} are needed, got {t.numel()} of {t.dtype}")
-    if t.get_device() != device or not t.is_contiguous():
-        _bad(f"{what}: a dense tensor on the current CUDA device is needed")
-    return t.data_ptr()
-
-
-def _device() -> int:
-    return _get_device() if _get_device is not None else torch.cuda.current_device()
-
-
-# Descriptors by what is in them: building one takes longer than the rest of a call.
-_scaled_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(ScaledDesc(*a)))
-_rows_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(RowsDesc(*a)))
-_norm_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(NormDesc(*a)))
-_logprobs_desc = functools.lru_cache(maxsize=4096)(lambda *a: ctypes.pointer(LogprobsDesc(*a)))
-_F32, _S8, _I64, _XCODES, _LOGITS = (torch.float32,), (torch.int8,), (torch.int64,), (torch.uint8, torch.int8), (torch.int32,) + _REAL
-
+# The four calls below check their tensors (shapes, types, strides, device: ValueError) and fill the descriptors in C++: csrc/f8_torch.cpp.
 
 def f8_linear_scaled(x, x_scale, w, w_scale, y, bias=None, stream=None):
     """y = x w^T of 8-bit codes, one real scale per row of x (or one for all) and per row of w (or one for all).
@@ -306,31 +262,16 @@ def f8_linear_scaled(x, x_scale, w, w_scale, y, bias=None, stream=None):
     x [n, k] uint8 or int8, w [out, k] int8, x_scale [n] or [1], w_scale [out] or [1] float32, bias [out] or None, y [n, out]
     float32, float16 or bfloat16; rows may be strided.
     """
-    dev = _device()
-    xp, ldx = _matrix(x, "x", None, _XCODES, dev)
-    wp, ldw = _matrix(w, "w", None, _S8, dev)
-    n, k = x.shape
-    out = w.shape[0]
-    if w.shape[1] != k:
-        _bad(f"w: rows of {k} codes are needed, got {w.shape[1]}")
-    yp, ldy = _matrix(y, "y", (n, out), _REAL, dev)
-    xs, ws, bp = _vector(x_scale, "x_scale", (n, 1), _F32, dev), _vector(w_scale, "w_scale", (out, 1), _F32, dev), _vector(bias, "bias", (out,), _REAL, dev)
-    d = _scaled_desc(n, k, out, _CODES[x.dtype], _CODES[y.dtype], _CODES[bias.dtype] if bias is not None else F8_F32,
-                     x_scale.numel(), w_scale.numel(), ldx, ldw, ldy)
-    _check(_lib.f8_linear_scaled(d, xp, xs, wp, ws, bp, yp, _stream(stream)))
+    status = _f8torch.linear_scaled(x, x_scale, w, w_scale, y, bias, stream)
+    if status:
+        _check(status)
 
 
 def f8_quantize_rows(x, q=None, scale=None, y=None, u=None, act=F8_ACT_NONE, stream=None):
     """Rows of act(x) * u to int8 codes q [n, c] with scale [n]; y: the values the codes stand for (without q: act(x) * u itself)."""
-    dev = _device()
-    xp, ldx = _matrix(x, "x", None, _REAL, dev)
-    shape, t = x.shape, (x.dtype,)
-    n, c = shape
-    up, ldu = _matrix(u, "u", shape, t, dev) if u is not None else (None, 0)
-    yp, ldy = _matrix(y, "y", shape, t, dev) if y is not None else (None, 0)
-    qp, ldq = _matrix(q, "q", shape, _S8, dev) if q is not None else (None, 0)
-    _check(_lib.f8_quantize_rows(_rows_desc(n, c, _CODES[x.dtype], act, ldx, ldu, ldy, ldq), xp, up, qp,
-                                 _vector(scale, "scale", (n,), _F32, dev), yp, _stream(stream)))
+    status = _f8torch.quantize_rows(x, q, scale, y, u, act, stream)
+    if status:
+        _check(status)
 
 
 def f8_norm_quantize(x, q=None, scale=None, y=None, *, residual=None, residual_out=None, gate=None, gate_act=F8_ACT_NONE,
@@ -340,25 +281,10 @@ def f8_norm_quantize(x, q=None, scale=None, y=None, *, residual=None, residual_o
 
     y: the values the codes stand for (without q: pre(t) itself).  gate [n, c] or [1, c]; norm weights [c] float32 or of x's type.
     """
-    dev = _device()
-    xp, ldx = _matrix(x, "x", None, _REAL, dev)
-    shape, t = x.shape, (x.dtype,)
-    n, c = shape
-    gp, ldg, gate_rows = None, 0, 1
-    if gate is not None:
-        gate_rows = gate.shape[0]
-        gp, ldg = _matrix(gate, "gate", (1 if gate_rows == 1 else n, c), t, dev)
-    rp, ldr = _matrix(residual, "residual", shape, t, dev) if residual is not None else (None, 0)
-    sp, lds = _matrix(residual_out, "residual_out", shape, t, dev) if residual_out is not None else (None, 0)
-    yp, ldy = _matrix(y, "y", shape, t, dev) if y is not None else (None, 0)
-    qp, ldq = _matrix(q, "q", shape, _S8, dev) if q is not None else (None, 0)
-    wt = next((v.dtype for v in (pre_w, post_w, pre_b, post_b) if v is not None), torch.float32)
-    if wt is not torch.float32 and wt is not x.dtype:
-        _bad(f"norm weights of {wt} with rows of {x.dtype}")
-    w = [_vector(v, "norm weights", (c,), (wt,), dev) for v in (post_w, post_b, pre_w, pre_b)]
-    d = _norm_desc(n, c, _CODES[x.dtype], _CODES[wt], post_norm, pre_norm, gate_act, gate_rows, eps, weight_offset, branch_scale,
-                   ldx, ldg, ldr, lds, ldy, ldq)
-    _check(_lib.f8_norm_quantize(d, xp, gp, rp, w[0], w[1], w[2], w[3], sp, qp, _vector(scale, "scale", (n,), _F32, dev), yp, _stream(stream)))
+    status = _f8torch.norm_quantize(x, q, scale, y, residual, residual_out, gate, gate_act, post_norm, post_w, post_b, pre_norm, pre_w, pre_b,
+                                    eps, weight_offset, branch_scale, stream)
+    if status:
+        _check(status)
 
 
 def f8_token_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_logprobs=None, top_ids=None, fl=0, inv_temperature=1.0, stream=None):
@@ -366,16 +292,9 @@ def f8_token_logprobs(logits, tokens=None, logprobs=None, entropy=None, top_logp
 
     int32 logits are codes with fl fractional bits, as a network's last layer gives them.
     """
-    dev = _device()
-    lp, ldl = _matrix(logits, "logits", None, _LOGITS, dev)
-    n, v = logits.shape
-    count = 0 if tokens is None else tokens.numel() // max(n, 1)
-    top = max((t.shape[-1] for t in (top_logprobs, top_ids) if t is not None), default=0)
-    d = _logprobs_desc(n, v, _CODES[logits.dtype], fl, count, top, inv_temperature, ldl)
-    _check(_lib.f8_token_logprobs(d, lp, _vector(tokens, "tokens", (n * count,), _I64, dev),
-                                  _vector(logprobs, "logprobs", (n * count,), _F32, dev), _vector(entropy, "entropy", (n,), _F32, dev),
-                                  _vector(top_logprobs, "top_logprobs", (n * top,), _F32, dev),
-                                  _vector(top_ids, "top_ids", (n * top,), _I64, dev), _stream(stream)))
+    status = _f8torch.token_logprobs(logits, tokens, logprobs, entropy, top_logprobs, top_ids, fl, inv_temperature, stream)
+    if status:
+        _check(status)
 
 
 def f8_conv_workspace_bytes(desc: ConvDesc) -> int:

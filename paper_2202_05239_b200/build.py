@@ -1,4 +1,4 @@
-"""Builds the CUDA library (``libf8net.so``) in-tree with nvcc for sm_100a."""
+"""Builds the CUDA library (``libf8net.so``) in-tree with nvcc for sm_100a, and the torch binding beside it with g++."""
 from __future__ import annotations
 
 import glob
@@ -8,6 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libf8net.so")
+BINDING = os.path.join(HERE, "_f8torch.so")
 
 
 def sources():
@@ -20,7 +21,35 @@ def _newest_source_mtime() -> float:
     return max(os.path.getmtime(f) for f in files)
 
 
+def build_binding(force: bool = False) -> str:
+    """The calls on torch tensors that are made from C++ (csrc/f8_torch.cpp), linked against torch and the library."""
+    source = os.path.join(CSRC, "f8_torch.cpp")
+    header = os.path.join(os.path.dirname(HERE), "include", "f8net.h")
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(os.path.getmtime(source), os.path.getmtime(header)):
+        return BINDING
+    import sysconfig
+
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    tmp = BINDING + ".tmp%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-o", tmp, source,
+                           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+                           "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+                           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(cuda, "include"),
+                           "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+                           "-L" + HERE, "-l:libf8net.so", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_library(force, verbose)
+    build_binding(force)
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
