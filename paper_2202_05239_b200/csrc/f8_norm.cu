@@ -129,31 +129,31 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
     __shared__ uint32_t urooms[2][32];
     using D = Deal<T, MODE, THREADS, E>;
     constexpr int PER = D::PER, PAIRS = D::PAIRS;
-    constexpr bool PIPE = MODE != LOOSE, KEEP = E == 8 && MODE != SHIFT;      // (shifted rows meet other weights from row to row)
+    constexpr bool PIPE = MODE != LOOSE, KEEP = E == 8;       // (rows of a block lie alike: they meet the same weights)
     const float per = 1.f / (float)p.c;
     const bool own_gate = p.gate && p.ldg, fold = !p.post_b;
     const int tensors = 1 + (p.res ? 1 : 0) + (own_gate ? 1 : 0), gate_at = tensors - 1;
     const Ring<BLOCK, PER> ring(smem, tensors);
-    const long long step = (long long)gridDim.x * GROUPS;
-    long long row = GROUPS == 1 ? blockIdx.x : (long long)(threadIdx.x / THREADS) * gridDim.x + blockIdx.x;
-    const T *nx = (const T *)p.x + row * p.ldx, *nr = (const T *)p.res + row * p.ldr, *ng = (const T *)p.gate + row * p.ldg;    // rows on their way
-    auto send = [&](bool some, int stage) {
-        if (some) {
-            const D d(nx, p.c);
+    const uint32_t step = gridDim.x * GROUPS, rows = (uint32_t)n;
+    uint32_t row = GROUPS == 1 ? blockIdx.x : threadIdx.x / THREADS * gridDim.x + blockIdx.x;
+    const uint32_t bx = (uint32_t)p.ldx * sizeof(T), br = (uint32_t)p.ldr * sizeof(T), bg = (uint32_t)p.ldg * sizeof(T);
+    const uint32_t bs = (uint32_t)p.lds * sizeof(T), by = (uint32_t)p.ldy * sizeof(T), bq = (uint32_t)p.ldq;
+    const D d(row_at((const T *)p.x, row, bx), p.c);
+    auto send = [&](uint32_t r, int stage) {
+        if (r < rows) {
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                d.send(nx, j, ring.place(stage, 0, j));
-                if (p.res) d.send(nr, j, ring.place(stage, 1, j));
-                if (own_gate) d.send(ng, j, ring.place(stage, gate_at, j));
+                d.send(row_at((const T *)p.x, r, bx), j, ring.place(stage, 0, j));
+                if (p.res) d.send(row_at((const T *)p.res, r, br), j, ring.place(stage, 1, j));
+                if (own_gate) d.send(row_at((const T *)p.gate, r, bg), j, ring.place(stage, gate_at, j));
             }
         }
         ring_commit();
-        nx += step * p.ldx;
-        nr += step * p.ldr;
-        ng += step * p.ldg;
     };
-    const T *cx = nx, *cr = nr, *cg = ng;          // the row at work
-    if (PIPE) send(row < n, 0);
+    if (PIPE) {
+        ring.clear(d);
+        send(row, 0);
+    }
     auto weight = [&](const void *w, int i) { return w ? (sizeof(T) == 4 || w32 ? ((const float *)w)[i] : to_float(((const T *)w)[i])) + p.weight_offset : 1.f; };
     // the factor of x / deviation in the residual sum: weight, beta and a shared gate (with a bias behind the post norm the weight alone)
     auto post_weight = [&](int i) {
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
         f *= p.branch_scale;
         return p.gate && !own_gate ? f * gate_value(to_float(((const T *)p.gate)[i]), p.gate_act) : f;
     };
-    auto factor = [&](const D &d, int j, F2 (&f)[PAIRS], bool post) {
+    auto factor = [&](int j, F2 (&f)[PAIRS], bool post) {
         float e[D::VEC];
 #pragma unroll
         for (int k = 0; k < D::VEC; ++k) {
@@ -174,11 +174,10 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
     };
     F2 kept[KEEP ? 2 : 1][PER][PAIRS];
     if (KEEP) {
-        const D d((const T *)p.x, p.c);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            factor(d, j, kept[0][j], true);
-            factor(d, j, kept[KEEP ? 1 : 0][j], false);
+            factor(j, kept[0][j], true);
+            factor(j, kept[KEEP ? 1 : 0][j], false);
         }
     }
     auto activate_gate = [&](F2 (&f)[PAIRS]) {
@@ -189,19 +188,16 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             f[i] = pair(gate_value(g.x, p.gate_act), gate_value(g.y, p.gate_act));
         }
     };
-    T *sum = (T *)p.sum + row * p.lds, *y = (T *)p.y + row * p.ldy;
-    int8_t *q = p.q + row * p.ldq;
-    for (int stage = 0; row < n; row += step, stage ^= 1) {
+    for (int stage = 0; row < rows; row += step, stage ^= 1) {
         float (*const room)[32] = rooms[stage];
         uint32_t *const uroom = urooms[stage];
-        const D d(cx, p.c);
         if (PIPE) {
-            send(row + step < n, stage ^ 1);
+            send(row + step, stage ^ 1);
             ring_wait();
         }
         F2 v[PER][PAIRS];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(cx, j), v[j]);
+        for (int j = 0; j < PER; ++j) unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(row_at((const T *)p.x, row, bx), j), v[j]);
         // v <- (v - mean) / deviation
         auto standardize = [&](int kind, float (*rm)[32]) {
             F2 s = 0ull;
@@ -235,7 +231,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 F2 f[PAIRS];
-                if (!KEEP) factor(d, j, f, post);
+                if (!KEEP) factor(j, f, post);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], KEEP ? kept[KEEP && !post ? 1 : 0][j][i] : f[i]);
             }
@@ -271,7 +267,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 F2 f[PAIRS];
-                unpack<T>(PIPE ? d.take(j, ring.place(stage, gate_at, j)) : d.load(cg, j), f);
+                unpack<T>(PIPE ? d.take(j, ring.place(stage, gate_at, j)) : d.load(row_at((const T *)p.gate, row, bg), j), f);
                 activate_gate(f);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
@@ -285,29 +281,21 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[i] = kept[0][j][i];
             } else if (fold) {
-                factor(d, j, f, true);
+                factor(j, f, true);
             } else {
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[i] = both(p.branch_scale);
             }
             if (p.res) {
-                unpack<T>(PIPE ? d.take(j, ring.place(stage, 1, j)) : d.load(cr, j), t);
+                unpack<T>(PIPE ? d.take(j, ring.place(stage, 1, j)) : d.load(row_at((const T *)p.res, row, br), j), t);
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[j][i] = fma2(v[j][i], f[i], t[i]);
             } else {
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
             }
-            if (p.sum) d.store(sum, j, v[j]);
+            if (p.sum) d.store(row_at((T *)p.sum, row, bs), j, v[j]);
         }
-        T *const my_y = y;
-        int8_t *const my_q = q;
-        cx += step * p.ldx;
-        cr += step * p.ldr;
-        cg += step * p.ldg;
-        sum += step * p.lds;
-        y += step * p.ldy;
-        q += step * p.ldq;
         if (!p.q && !p.y) continue;
         float peak = 0.f;
         uint32_t top;
@@ -350,7 +338,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             }
             if (!p.q) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) d.store(my_y, j, v[j]);
+                for (int j = 0; j < PER; ++j) d.store(row_at((T *)p.y, row, by), j, v[j]);
                 continue;
             }
 #pragma unroll
@@ -366,7 +354,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
         }
         const RowScale s = RowScale::of_warp(top);
         if (threadIdx.x % THREADS == 0) p.scale[row] = s.scale;
-        emit<T>(d, v, s, top < 0x7f800000u, my_q, p.y ? my_y : nullptr);
+        emit<T>(d, v, s, top < 0x7f800000u, row_at(p.q, row, bq), p.y ? row_at((T *)p.y, row, by) : nullptr);
     }
 }
 
@@ -404,9 +392,11 @@ cudaError_t launch_norm(const NormParams &p, long long n, bool w32, cudaStream_t
     l.vector(p.post_b);
     l.vector(p.pre_w);
     l.vector(p.pre_b);
-    if (l.same && !l.shift() && p.c <= ROW_MOST) return launch_row_norm<T, PLAIN>(p, w32, n, st);
-    if (l.same && p.c + VEC - 1 <= ROW_MOST) return launch_row_norm<T, SHIFT>(p, w32, n, st);
-    if (p.c <= ROW_MOST) return launch_row_norm<T, LOOSE>(p, w32, n, st);
+    if (l.near) {
+        if (l.same && !l.shift() && p.c <= ROW_MOST) return launch_row_norm<T, PLAIN>(p, w32, n, st);
+        if (l.same && p.c + VEC - 1 <= ROW_MOST) return launch_row_norm<T, SHIFT>(p, w32, n, st);
+        if (p.c <= ROW_MOST) return launch_row_norm<T, LOOSE>(p, w32, n, st);
+    }
     const dim3 grid((unsigned)n);
     if (w32) return launch_early(long_norm_kernel<T, float>, grid, ROW_THREADS, 0, st, p);
     return launch_early(long_norm_kernel<T, T>, grid, ROW_THREADS, 0, st, p);

@@ -132,11 +132,11 @@ struct Deal {
     __device__ __forceinline__ void send(const T *row, int j, uint32_t place) const {
         if (on(j)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place), "l"(row + at(j, 0)) : "memory");
     }
+    // (places that nothing is sent to hold zeros, see Ring::clear)
     __device__ __forceinline__ uint4 take(int j, uint32_t place) const {
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (!on(j)) return w;
+        uint4 w;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place) : "memory");
-        if (!whole(j)) {
+        if (MODE == SHIFT && !whole(j)) {
 #pragma unroll
             for (int k = 0; k < VEC; ++k)
                 if (!in(j, k)) set_element<T>(w, k, 0u);
@@ -226,6 +226,13 @@ __device__ __forceinline__ void emit(const D &d, F2 (&v)[D::PER][D::PAIRS], cons
     }
 }
 
+// Row `row` of a matrix whose rows are `bytes` apart: one multiply-add of two 32-bit numbers (the kernels for rows in registers take
+// distances below 2^32 bytes).
+template <typename T> __device__ __forceinline__ T *row_at(T *base, uint32_t row, uint32_t bytes) { return (T *)((char *)base + (unsigned long long)row * bytes); }
+template <typename T> __device__ __forceinline__ const T *row_at(const T *base, uint32_t row, uint32_t bytes) {
+    return (const T *)((const char *)base + (unsigned long long)row * bytes);
+}
+
 __host__ __device__ constexpr int row_block(int threads) { return threads == 32 ? 128 : threads; }      // a warp a row: four rows in a block
 // blocks of an SM that the registers have to leave room for (64 a thread)
 constexpr int row_blocks(int threads) { return 1024 / row_block(threads); }
@@ -237,6 +244,15 @@ struct Ring {
     uint32_t mine;
     int tensors;
     __device__ __forceinline__ Ring(const void *smem, int tensors_) : mine((uint32_t)__cvta_generic_to_shared(smem) + threadIdx.x * 16u), tensors(tensors_) {}
+    // zeros where no row of this block has an element
+    template <typename D>
+    __device__ __forceinline__ void clear(const D &d) const {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (!d.on(j))
+                for (int i = 0; i < 2 * tensors; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(mine + (uint32_t)((i * PER + j) * BLOCK * 16)), "r"(0) : "memory");
+    }
     __device__ __forceinline__ uint32_t place(int stage, int tensor, int j) const { return mine + (uint32_t)(((stage * tensors + tensor) * PER + j) * BLOCK * 16); }
 };
 __device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -246,7 +262,7 @@ __device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group 
 struct RowLayout {
     long long n;
     int size, vec;
-    bool first = true, same = true, whole = true;
+    bool first = true, same = true, whole = true, near = true;
     uintptr_t base = 0, step = 0;
     RowLayout(long long n_, int size_, int c) : n(n_), size(size_), vec(16 / size_) { whole = c % vec == 0; }
     // a matrix of `bytes` a element and a distance of ld elements between its rows
@@ -255,6 +271,7 @@ struct RowLayout {
         const uintptr_t b = (uintptr_t)p / bytes % vec, s = n > 1 ? (uintptr_t)ld % vec : 0;
         if (first) { base = b; step = s; first = false; }
         same = same && b == base && s == step;
+        near = near && ld * bytes < (1ll << 32);
     }
     void vector(const void *p) { whole = whole && ((uintptr_t)p & 15) == 0; }
     int shift() const { return base != 0 || step != 0 || !whole; }
@@ -266,6 +283,7 @@ struct RingFit { std::atomic<int> held[64][4]; };
 constexpr size_t RING_MOST = 220 * 1024;
 inline size_t ring_bytes(int threads, int per, int tensors) { return (size_t)2 * tensors * per * row_block(threads) * 16; }
 
+// Where there are more rows than blocks hold, the blocks are a multiple of eight, so that a block's rows all lie alike (SHIFT).
 template <auto KERNEL, typename... A>
 cudaError_t launch_ring(int threads, int per, int tensors, long long n, cudaStream_t st, A... a) {
     static RingFit fit;
@@ -283,7 +301,7 @@ cudaError_t launch_ring(int threads, int per, int tensors, long long n, cudaStre
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, (const void *)KERNEL, block, smem);
         if (e != cudaSuccess) return e;
-        held = std::max(blocks, 1) * sms;
+        held = std::max(std::max(blocks, 1) * sms / 8 * 8, 8);
         fit.held[dev][tensors].store(held, std::memory_order_relaxed);
     }
     const long long blocks = threads == 32 ? (n + 3) / 4 : n;

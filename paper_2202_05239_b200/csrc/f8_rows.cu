@@ -62,25 +62,26 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
     __shared__ uint32_t room[2][32];
     using D = Deal<T, MODE, THREADS, E>;
     constexpr int PER = D::PER, PAIRS = D::PAIRS;
-    const long long step = (long long)gridDim.x * (THREADS == 32 ? 4 : 1);
-    long long row = THREADS == 32 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    const uint32_t step = gridDim.x * (THREADS == 32 ? 4 : 1), rows = (uint32_t)n;
+    uint32_t row = THREADS == 32 ? (threadIdx.x >> 5) * gridDim.x + blockIdx.x : blockIdx.x;
+    const uint32_t bx = (uint32_t)p.ldx * sizeof(T), bu = (uint32_t)p.ldu * sizeof(T), by = (uint32_t)p.ldy * sizeof(T), bq = (uint32_t)p.ldq;
+    const D d(row_at((const T *)p.x, row, bx), p.c);
     const Ring<row_block(THREADS), PER> ring(smem, p.u ? 2 : 1);
-    auto send = [&](long long r, int stage) {
-        if (r < n) {
-            const T *x = (const T *)p.x + r * p.ldx;
-            const D d(x, p.c);
+    auto send = [&](uint32_t r, int stage) {
+        if (r < rows) {
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                d.send(x, j, ring.place(stage, 0, j));
-                if (p.u) d.send((const T *)p.u + r * p.ldu, j, ring.place(stage, 1, j));
+                d.send(row_at((const T *)p.x, r, bx), j, ring.place(stage, 0, j));
+                if (p.u) d.send(row_at((const T *)p.u, r, bu), j, ring.place(stage, 1, j));
             }
         }
         ring_commit();
     };
-    if (PIPE) send(row, 0);
-    for (int stage = 0; row < n; row += step, stage ^= 1) {
-        const T *x = (const T *)p.x + row * p.ldx, *u = p.u ? (const T *)p.u + row * p.ldu : nullptr;
-        const D d(x, p.c);
+    if (PIPE) {
+        ring.clear(d);
+        send(row, 0);
+    }
+    for (int stage = 0; row < rows; row += step, stage ^= 1) {
         if (PIPE) {
             send(row + step, stage ^ 1);
             ring_wait();
@@ -90,8 +91,8 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
         float peak = 0.f;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(x, j), v[j]);
-            if (!PIPE && u) ru[j] = d.load(u, j);
+            unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(row_at((const T *)p.x, row, bx), j), v[j]);
+            if (!PIPE && p.u) ru[j] = d.load(row_at((const T *)p.u, row, bu), j);
         }
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
                     v[j][i] = pair(activate_row<T>(f.x, p.act), activate_row<T>(f.y, p.act));
                 }
             }
-            if (u) {
+            if (p.u) {
                 F2 f[PAIRS];
                 unpack<T>(PIPE ? d.take(j, ring.place(stage, 1, j)) : ru[j], f);
 #pragma unroll
@@ -111,7 +112,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i) peak = peak_of(peak, v[j][i]);
         }
-        T *y = p.y ? (T *)p.y + row * p.ldy : nullptr;
+        T *y = p.y ? row_at((T *)p.y, row, by) : nullptr;
         if (!p.q) {
 #pragma unroll
             for (int j = 0; j < PER; ++j) d.store(y, j, v[j]);
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
         const uint32_t top = block_reduce<THREADS>(magnitude(peak), UMaxOp(), room[stage]);
         const RowScale s = RowScale::of_warp(top);
         if ((THREADS == 32 ? threadIdx.x & 31 : threadIdx.x) == 0) p.scale[row] = s.scale;
-        emit<T>(d, v, s, top < 0x7f800000u, p.q + row * p.ldq, y);
+        emit<T>(d, v, s, top < 0x7f800000u, row_at(p.q, row, bq), y);
     }
 }
 
@@ -157,7 +158,7 @@ cudaError_t launch_rows_act(const RowsParams &p, long long n, cudaStream_t st) {
 }
 template <typename T>
 cudaError_t launch_rows(const RowsParams &p, long long n, cudaStream_t st) {
-    if (p.c <= ROW_MOST) return p.act == F8_ACT_NONE ? launch_rows_act<T, false>(p, n, st) : launch_rows_act<T, true>(p, n, st);
+    if (p.c <= ROW_MOST && std::max({p.ldx, p.ldu, p.ldy, p.ldq}) * (long long)sizeof(T) < (1ll << 32)) return p.act == F8_ACT_NONE ? launch_rows_act<T, false>(p, n, st) : launch_rows_act<T, true>(p, n, st);
     const dim3 grid((unsigned)n);
     switch (p.act) {
         case F8_ACT_SILU: return launch_early(long_quantize_kernel<T, F8_ACT_SILU>, grid, ROW_THREADS, 0, st, p);
