@@ -360,7 +360,7 @@ f8_status f8_format_study_fixed(const float *x, long long n, int is_unsigned, do
  *     y[i, j] = round( fma( (float)acc * x_scale[i], w_scale[j], bias[j] ) )       float arithmetic, one rounding per operation
  *   x [n, k] F8_U8 or F8_S8, w [out, k] int8; x_scale [x_scales], x_scales n or 1 (one scale for all rows); w_scale [w_scales],
  *   w_scales out or 1; bias [out] of bias_dtype or NULL; y [n, out] of y_dtype (F8_F32, F8_F16, F8_BF16).
- * Errors: F8_ERR_NULL, F8_ERR_SHAPE, F8_ERR_DTYPE, F8_ERR_ALIGN (element alignment), F8_ERR_ACC_BOUND (k * 255 * 128, or
+ * Errors: F8_ERR_NULL, F8_ERR_SHAPE (also n or out above 2^31 - 256), F8_ERR_DTYPE, F8_ERR_ALIGN (element alignment), F8_ERR_ACC_BOUND (k * 255 * 128, or
  * k * 128 * 128 for signed x, reaches 2^31), F8_ERR_TIMEOUT. */
 typedef struct {
     int n, k, out;

@@ -238,7 +238,6 @@ f8_status run_dense(const F8ConvGeom &g, const F8Requant &q, const void *x, cons
 f8_status f8_set_error(f8_status s, const char *message) { return fail(s, "%s", message); }
 
 unsigned f8_plan_options_off() { return g_plan_off; }
-bool f8_force_direct() { return g_force_direct; }
 unsigned long long f8_wait_limit_cycles() { return g_wait_limit_cycles; }
 int *f8_last_plan_info() { return g_last_plan; }
 

@@ -170,6 +170,3 @@ f8_status f8_set_error(f8_status s, const char *message);
 
 // F8_OK, or F8_ERR_TIMEOUT (with its message) while the record of a wait that a kernel gave up is pending.
 f8_status f8_pending_timeout();
-
-// Test hook f8_debug_force_direct.
-bool f8_force_direct();

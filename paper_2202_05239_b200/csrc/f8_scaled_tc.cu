@@ -16,11 +16,74 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstring>
 
-#include "f8_scaled.h"
+#include "f8_real.cuh"
 #include "f8_tc_ptx.cuh"
 
 namespace {
+
+struct ScaledParams {
+    int n, k, out;
+    int y_dtype, bias_dtype;
+    int x_scales, w_scales;
+    long long ldx, ldw, ldy;
+    const uint8_t *x, *w;
+    const float *xs, *ws;
+    const void *bias;
+    void *y;
+};
+
+__device__ __forceinline__ float load_real(const void *p, int dtype, long long i) {
+    return dtype == F8_F32 ? ((const float *)p)[i] : dtype == F8_F16 ? to_float(((const __half *)p)[i]) : to_float(((const __nv_bfloat16 *)p)[i]);
+}
+__device__ __forceinline__ void store_real(void *p, int dtype, long long i, float v) {
+    if (dtype == F8_F32) ((float *)p)[i] = v;
+    else if (dtype == F8_F16) ((__half *)p)[i] = from_float<__half>(v);
+    else ((__nv_bfloat16 *)p)[i] = from_float<__nv_bfloat16>(v);
+}
+__device__ __forceinline__ float scaled(int acc, float sx, float sw, float b) { return __fmaf_rn(__fmul_rn(__int2float_rn(acc), sx), sw, b); }
+
+// Bytes sh .. sh + 15 of two neighbouring granules of 16 bytes: by words, then by bytes.
+__device__ __forceinline__ uint4 shift_bytes(uint4 a, uint4 b, uint32_t sh) {
+    if (sh & 8u) { a.x = a.z; a.y = a.w; a.z = b.x; a.w = b.y; b.x = b.z; b.y = b.w; }
+    if (sh & 4u) { a.x = a.y; a.y = a.z; a.z = a.w; a.w = b.x; b.x = b.y; }
+    const uint32_t bits = (sh & 3u) * 8u;
+    return make_uint4(__funnelshift_r(a.x, a.y, bits), __funnelshift_r(a.y, a.z, bits), __funnelshift_r(a.z, a.w, bits), __funnelshift_r(a.w, b.x, bits));
+}
+// The first n bytes, zeros behind them.
+__device__ __forceinline__ uint4 first_bytes(uint4 v, int n) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int m = n - 4 * j;
+        w[j] = m >= 4 ? w[j] : m <= 0 ? 0u : w[j] & (0xffffffffu >> (32 - 8 * m));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Four neighbouring outputs from their sums; `wide`: y may be written in words of four elements here.
+__device__ __forceinline__ void store_scaled4(const ScaledParams &p, const int (&acc)[4], int m, int o, float sx, const float (&sw)[4], const float (&b)[4], bool wide) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = scaled(acc[k], sx, sw[k], b[k]);
+    const long long at = (long long)m * p.ldy + o;
+    if (wide) {
+        if (p.y_dtype == F8_F32) {
+            *(float4 *)((float *)p.y + at) = make_float4(v[0], v[1], v[2], v[3]);
+        } else if (p.y_dtype == F8_F16) {
+            const __half2 a = __floats2half2_rn(v[0], v[1]), c = __floats2half2_rn(v[2], v[3]);
+            *(uint2 *)((__half *)p.y + at) = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&c);
+        } else {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), c = __floats2bfloat162_rn(v[2], v[3]);
+            *(uint2 *)((__nv_bfloat16 *)p.y + at) = make_uint2(*(const uint32_t *)&a, *(const uint32_t *)&c);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (o + k < p.out) store_real(p.y, p.y_dtype, at + k, v[k]);
+    }
+}
 
 constexpr int SC_KB = 128;                     // bytes of K in a chunk: one span of the swizzle
 constexpr int SC_MAX_STAGES = 24;
@@ -51,6 +114,7 @@ __device__ __forceinline__ uint4 cluster_load(uint32_t a) {
 struct SplitParams {
     ScaledParams s;
     int m_tiles, chunks, split, stages, a_rows;      // a_rows: rows of x a copy brings, a multiple of 8
+    int soft_warps, slots;         // without bulk copies: warps that fetch, chunks on their way (4 or 8)
     uint32_t idesc;
     uint64_t desc;
     bool wide;
@@ -58,35 +122,40 @@ struct SplitParams {
     unsigned long long wait_limit;
 };
 
-constexpr int SPLIT_THREADS = 192;            // producer, issuer, four warps that read the accumulator
+// Producer, issuer, four warps that read the accumulator; where bulk copies cannot fetch the operands (rows that do not start at multiples of
+// 16 bytes: an odd K, a slice), up to sixteen more warps do: the granules of 16 bytes that hold a row's chunk come through raw slots in shared
+// memory, are shifted together and written where the swizzle would put them.
+constexpr int SPLIT_THREADS = 192, SOFT_THREADS = 512;
+constexpr uint32_t SOFT_RAW = 16 * 144;       // bytes of a warp's slot: sixteen rows, nine granules each
 
-template <int BN>
-__global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+template <int BN, bool SOFT>
+__global__ void __launch_bounds__(SPLIT_THREADS + (SOFT ? SOFT_THREADS : 0), 1) scaled_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                                                                         const SplitParams p) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *const base = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     ScControl &ctl = *(ScControl *)base;
     float *const sw = (float *)(base + SC_CONTROL), *const bias = sw + BN, *const sx = bias + BN;     // of this tile
     uint8_t *const ring = base + 2 * SC_CONTROL + 1024;
-    const uint32_t ring_at = smem_u32(ring), full = smem_u32(&ctl.full[0]), empty = smem_u32(&ctl.empty[0]), tfull = smem_u32(&ctl.tfull[0]);
+    const uint32_t a_bytes = (uint32_t)p.a_rows * SC_KB, stage_bytes = a_bytes + BN * SC_KB;
+    const uint32_t raw_at = smem_u32(ring), ring_at = raw_at + (SOFT ? ((uint32_t)(p.slots * p.soft_warps) * SOFT_RAW + 1023u) & ~1023u : 0u);
+    const uint32_t full = smem_u32(&ctl.full[0]), empty = smem_u32(&ctl.empty[0]), tfull = smem_u32(&ctl.tfull[0]);
     const int warp = uniform((int)(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const int tile = (int)blockIdx.x / p.split, rank = (int)blockIdx.x % p.split;
     const int n_t = tile / p.m_tiles, m0 = (tile - n_t * p.m_tiles) * 128, n0 = n_t * BN;
     const int c0 = (int)((long long)p.chunks * rank / p.split), uses = (int)((long long)p.chunks * (rank + 1) / p.split) - c0;
-    const uint32_t a_bytes = (uint32_t)p.a_rows * SC_KB, stage_bytes = a_bytes + BN * SC_KB;
     const WaitCtx wc = make_wait_ctx(&ctl.abort_flag, p.status, p.wait_limit);
 
     if (threadIdx.x == 0) {
         ctl.abort_flag = 0;
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(full + 8 * s, 1);
+            mbar_init(full + 8 * s, SOFT ? p.soft_warps : 1);
             mbar_init(empty + 8 * s, 1);
         }
         mbar_init(tfull, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        prefetch_tensormap(&map_x);
-        prefetch_tensormap(&map_w);
+        if (!SOFT) prefetch_tensormap(&map_x);
+        if (!SOFT) prefetch_tensormap(&map_w);
     }
     if (warp == 1) tmem_alloc(smem_u32(&ctl.tmem), BN);
     tc_fence_before();
@@ -96,7 +165,79 @@ __global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __
     grid_dependency_wait();                    // the weights may come from earlier work in the stream as well
     grid_launch_dependents();
 
-    if (warp == 0) {
+    if (SOFT && warp >= SPLIT_THREADS / 32) {
+        // sixteen rows of the stage a warp: each chunk's nine granules of a row (one more than a chunk, for the shift) go to a raw slot of the
+        // warp's own, as many chunks ahead as there are slots; then eight lanes a row shift and write them.
+        const int pw = warp - SPLIT_THREADS / 32;
+        if (pw < p.soft_warps) {
+            const int all = p.a_rows + BN, r0 = 16 * pw;
+            auto row_of = [&](int r) -> const uint8_t * {           // a row of the stage, null where the matrices have none
+                r += r0;
+                if (r < p.a_rows) return m0 + r < p.s.n ? p.s.x + (long long)(m0 + r) * p.s.ldx : nullptr;
+                r -= p.a_rows;
+                return r < BN && n0 + r < p.s.out ? p.s.w + (long long)(n0 + r) * p.s.ldw : nullptr;
+            };
+            const int j = lane & 7, q0 = lane >> 3;
+            const uint8_t *src[5];                                  // granule j of rows q0, q0 + 4, .. ; the ninth granule of row `lane`
+            uint32_t sh = 0;                                        // a byte each: the rows' distance from a multiple of 16
+            int from[5];                                            // byte of the row at which the granule starts, in chunk 0 of this block
+#pragma unroll
+            for (int q = 0; q < 5; ++q) {
+                const uint8_t *const row = row_of(q < 4 ? q0 + 4 * q : lane & 15);
+                const uint32_t d = (uint32_t)(uintptr_t)row & 15u;
+                if (q < 4) sh |= d << (8 * q);
+                from[q] = c0 * SC_KB + (q < 4 ? 16 * j : 128) - (int)d;
+                src[q] = row + from[q];
+                // nothing to fetch: beyond every chunk
+                if (!row || (q == 4 && (lane >= 16 || d == 0))) {
+                    src[q] = p.s.w;
+                    from[q] = 0x7fffffff - SC_KB * 4096;
+                }
+            }
+            const uint32_t raw = raw_at + (uint32_t)pw * SOFT_RAW, slot_bytes = (uint32_t)p.soft_warps * SOFT_RAW;
+            const uint32_t ninth = raw + (uint32_t)(lane & 15) * 144u + 128u, mine = raw + (uint32_t)q0 * 144u + 16u * j;
+            auto fetch = [&](int u, int slot) {
+                if (u < uses) {
+#pragma unroll
+                    for (int q = 0; q < 5; ++q) {
+                        if (q == 4 && lane >= 16) break;
+                        const bool some = from[q] + u * SC_KB < p.s.k;
+                        const uint8_t *const g = some ? src[q] + (long long)u * SC_KB : (const uint8_t *)((uintptr_t)p.s.w & ~(uintptr_t)15);
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((q < 4 ? mine + 576u * q : ninth) + (uint32_t)slot * slot_bytes), "l"(g),
+                                     "r"(some ? 16 : 0)
+                                     : "memory");
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            for (int u = 0; u < p.slots - 1; ++u) fetch(u, u);
+            int stage = 0, slot = 0;
+            uint32_t phase = 0;
+            for (int u = 0; u < uses; ++u) {
+                fetch(u + p.slots - 1, slot == 0 ? p.slots - 1 : slot - 1);
+                if (p.slots == 8) asm volatile("cp.async.wait_group 7;" ::: "memory");
+                else asm volatile("cp.async.wait_group 3;" ::: "memory");
+                __syncwarp();
+                if (u >= p.stages && !warp_wait(empty + 8 * stage, phase ^ 1, wc, 153)) break;
+                const uint32_t dst = ring_at + (uint32_t)stage * stage_bytes + (uint32_t)r0 * SC_KB;       // (rows of x, then of w: one behind the other)
+                const int left = p.s.k - (c0 + u) * SC_KB - 16 * j;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = q0 + 4 * q;
+                    const uint32_t at = mine + 576u * q + (uint32_t)slot * slot_bytes;
+                    uint4 v = shift_bytes(lds128(at), lds128(at + 16), (sh >> (8 * q)) & 15u);
+                    if (left < 16) v = first_bytes(v, left);
+                    if (r0 + r < all) sts128(dst + (uint32_t)r * SC_KB + (((uint32_t)j ^ ((uint32_t)r & 7u)) << 4), v);
+                }
+                __syncwarp();                   // the slot is read: it may be filled again
+                if (lane == 0) mbar_arrive(full + 8 * stage);
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+                if (++slot == p.slots) slot = 0;
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        }
+    } else if (SOFT && warp == 0) {
+    } else if (warp == 0) {
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -120,6 +261,9 @@ __global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __
         const uint32_t desc_hi = (uint32_t)(p.desc >> 32);
         for (int u = 0; u < uses; ++u) {
             if (!warp_wait(full + 8 * stage, phase, wc, 151)) break;
+            // what the warps wrote, for the tensor cores to read (the fence stands here, behind the barrier: in the writers it would wait for
+            // the loads they have on their way)
+            if (SOFT) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_fence_after();
             const uint32_t lo = (uint32_t)p.desc | (((ring_at + (uint32_t)stage * stage_bytes) & 0x3ffffu) >> 4);
             mma_i8_sub<4>(tmem, lo, lo + (a_bytes >> 4), desc_hi, p.idesc, u != 0 ? 1u : 0u);
@@ -132,7 +276,7 @@ __global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __
         }
         __syncwarp();
     } else {
-        const int t = (int)threadIdx.x - 64;
+        const int t = (int)threadIdx.x - 64;      // 0 .. 127
         for (int i = t; i < BN; i += 128) {
             const int o = n0 + i;
             sw[i] = o < p.s.out ? p.s.ws[p.s.w_scales == 1 ? 0 : o] : 0.f;
@@ -140,8 +284,8 @@ __global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __
         }
         sx[t] = m0 + t < p.s.n ? p.s.xs[p.s.x_scales == 1 ? 0 : m0 + t] : 0.f;
     }
-    // every warp waits for the accumulator: behind it the ring is free
-    if (warp >= 2) {
+    // the accumulator is complete: the ring is free, and takes the partial sums
+    if (warp >= 2 && warp < 6) {
         warp_wait(tfull, 0, wc, 152);
         tc_fence_after();
         const int rows = min(128, p.s.n - m0), row = 32 * (warp & 3) + lane;
@@ -169,7 +313,7 @@ __global__ void __launch_bounds__(SPLIT_THREADS, 1) scaled_split_kernel(const __
     {
         const int rows = min(128, p.s.n - m0), all = rows * (BN / 4);
         const int from = (int)((long long)all * rank / p.split), to = (int)((long long)all * (rank + 1) / p.split);
-        for (int i = from + (int)threadIdx.x; i < to; i += SPLIT_THREADS) {
+        for (int i = from + (int)threadIdx.x; i < to; i += (int)blockDim.x) {
             const int row = i / (BN / 4), c = (i - row * (BN / 4)) * 4, o = n0 + c;
             if (o >= p.s.out) continue;
             const uint32_t at = ring_at + (uint32_t)(row * (BN + 4) + c) * 4;
@@ -456,7 +600,7 @@ bool wide_rows(const ScaledParams &p) {
     return ((uintptr_t)p.y & (uintptr_t)(4 * size - 1)) == 0 && (p.n == 1 || (p.ldy & 3) == 0);
 }
 
-template <int BN>
+template <int BN, bool SOFT>
 cudaError_t launch_split(const ScaledParams &s, bool x_signed, int split, int *status, int dev, cudaStream_t st) {
     SplitParams p;
     p.s = s;
@@ -465,10 +609,13 @@ cudaError_t launch_split(const ScaledParams &s, bool x_signed, int split, int *s
     p.split = split;
     p.a_rows = std::min(128, (s.n + 7) / 8 * 8);
     const int tiles = p.m_tiles * ((s.out + BN - 1) / BN), uses = (p.chunks + split - 1) / split;
-    const size_t stage = (size_t)(p.a_rows + BN) * SC_KB, head = 3 * 1024, slack = (size_t)(128 - p.a_rows) * SC_KB;
+    p.soft_warps = (p.a_rows + BN + 15) / 16;
+    p.slots = p.soft_warps <= 9 ? 8 : 4;
+    const size_t raw = SOFT ? ((size_t)p.slots * p.soft_warps * SOFT_RAW + 1023) / 1024 * 1024 : 0;
+    const size_t stage = (size_t)(p.a_rows + BN) * SC_KB, head = 3 * 1024 + raw, slack = (size_t)(128 - p.a_rows) * SC_KB;
     const size_t partial = (size_t)std::min(128, s.n) * (BN + 4) * 4;
     // a block to an SM gets a ring of its whole share if that fits; two to an SM get half the memory each
-    const size_t room = (tiles * split > sm_count(dev) ? SC_SMEM / 2 - 1024 : SC_SMEM) - head - slack;
+    const size_t room = (!SOFT && tiles * split > sm_count(dev) ? SC_SMEM / 2 - 1024 : SC_SMEM) - head - slack;
     p.stages = std::max(1, std::min({uses, SC_MAX_STAGES, (int)(room / stage)}));
     const size_t smem = 1024 + head + std::max(p.stages * stage + slack, partial);
     p.idesc = (2u << 4) | ((x_signed ? 1u : 0u) << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | (8u << 24);
@@ -477,10 +624,15 @@ cudaError_t launch_split(const ScaledParams &s, bool x_signed, int split, int *s
     p.status = status;
     p.wait_limit = f8_wait_limit_cycles();
     CUtensorMap mx, mw;
-    if (!encode(&mx, s.x, s.n, s.k, s.ldx, p.a_rows) || !encode(&mw, s.w, s.out, s.k, s.ldw, BN)) return cudaErrorNotSupported;
-    const cudaError_t e = allow_smem<scaled_split_kernel<BN>>(dev);
+    if (SOFT) {
+        memset(&mx, 0, sizeof(mx));
+        memset(&mw, 0, sizeof(mw));
+    } else if (!encode(&mx, s.x, s.n, s.k, s.ldx, p.a_rows) || !encode(&mw, s.w, s.out, s.k, s.ldw, BN)) {
+        return cudaErrorNotSupported;
+    }
+    const cudaError_t e = allow_smem<scaled_split_kernel<BN, SOFT>>(dev);
     if (e != cudaSuccess) return e;
-    return launch_clusters(scaled_split_kernel<BN>, tiles * split, split, SPLIT_THREADS, smem, st, mx, mw, p);
+    return launch_clusters(scaled_split_kernel<BN, SOFT>, tiles * split, split, SPLIT_THREADS + (SOFT ? SOFT_THREADS : 0), smem, st, mx, mw, p);
 }
 
 cudaError_t launch_pairs(const ScaledParams &s, bool x_signed, int *status, int dev, cudaStream_t st) {
@@ -527,25 +679,31 @@ cudaError_t launch_pairs(const ScaledParams &s, bool x_signed, int *status, int 
 
 // Which kernel and tile, by an estimate of the time in microseconds, fitted to calls of 1 to 8192 rows on a B200 (within 15 % of most):
 //   split   3.3 for the launch, then the slower of the blocks' chunks (one of BN columns takes 0.12 or 0.15, plus the rows of x it
-//           brings; more blocks than SMs share them) and the memory (5.7 or 6.2 TB/s, if enough SMs ask), then the tile's way out, and for a split the
-//           exchange.  Eight blocks of a cluster only pay with few rows and no more blocks than SMs.
+//           brings; more blocks than SMs share them) and the memory (5.7 or 6.2 TB/s, if enough SMs ask), then the tile's way out, and for a split
+//           the exchange.  Eight blocks of a cluster only pay with few rows and no more blocks than SMs.
+//   soft    (rows fetched by warps) one block to an SM, 0.55 or 0.72 a chunk and the rows of x
 //   pairs   7, then rounds of tiles of 0.29 a chunk, at least 3 for the tile's way out
 // Measured (us): 1 x 4096 x 4096 split by 1 / 2 / 4 / 8 at 64 columns 8.3 / 7.2 / 6.7 / 7.7; 256 x 2048 x 1000 7.9 / 6.5 / 5.4 / 7.7; 1 x 8192 x 28672
-// 64 columns 42.6, 128 columns 38.7; 512 x 4096 x 4096 split 15.1, pairs 15.5; 1024 x 4096 x 4096 split 21.9, pairs 16.9.
+// 64 columns 42.6, 128 columns 38.7; 512 x 4096 x 4096 split 15.1, pairs 15.5; 1024 x 4096 x 4096 split 21.9, pairs 16.9; soft 1 x 4097 x 4096 at 128
+// columns 28.8 / 17.6 / 13.0 / 26.5, 4096 x 4097 x 8192 64 columns 872, 128 columns 529.
 struct ScaledCut { int bn, split; };
-ScaledCut scaled_cut(const ScaledParams &s, int sms) {
-    const double chunks = (s.k + SC_KB - 1) / SC_KB, m_tiles = (s.n + 127) / 128, rows = std::min(128, (s.n + 7) / 8 * 8);
+ScaledCut scaled_cut(const ScaledParams &s, int sms, bool soft) {
+    const double chunks = (s.k + SC_KB - 1) / SC_KB, m_tiles = ((long long)s.n + 127) / 128, rows = std::min(128ll, ((long long)s.n + 7) / 8 * 8);
     const double bytes = (double)s.n * s.k + (double)s.out * s.k + (double)s.n * s.out * real_size(s.y_dtype);
-    const double pair_tiles = (double)((s.n + 255) / 256) * ((s.out + 255) / 256);
+    const double pair_tiles = (double)(((long long)s.n + 255) / 256) * (((long long)s.out + 255) / 256);
     ScaledCut best = {256, 1};
-    double least = 7.0 + std::ceil(pair_tiles / (sms / 2)) * std::max(chunks * 0.29, 3.0);
+    double least = soft ? 1e300 : 7.0 + std::ceil(pair_tiles / (sms / 2)) * std::max(chunks * 0.29, 3.0);
     for (int bn = 64; bn <= 128; bn *= 2) {
-        const double tiles = m_tiles * ((s.out + bn - 1) / bn), chunk = bn == 64 ? 0.115 + 0.0009 * rows : 0.15 + 0.0013 * rows;
-        if (tiles > 1e6) continue;
-        for (int split = 1; split <= 8 && (split == 1 || chunks >= 4 * split); split *= 2) {
-            const double share = tiles * split / sms, load = std::max(share, 1.0);
-            const double stream = std::max(load * std::ceil(chunks / split) * chunk, bytes / (bn == 64 ? 5.7e6 : 6.2e6) / std::min(share, 1.0));
-            double t = 3.3 + stream + load * 1.1 * rows * bn / 8192 / split;
+        const double tiles = m_tiles * (((long long)s.out + bn - 1) / bn), out = 1.1 * rows * bn / 8192;
+        for (int split = 1; split <= 8 && (split == 1 || chunks >= (soft ? 1 : 4) * split); split *= 2) {
+            const double share = tiles * split / sms, load = std::max(share, 1.0), uses = std::ceil(chunks / split);
+            double t;
+            if (soft) {
+                t = 0.5 + std::ceil(share) * (3.0 + uses * (bn == 64 ? 0.55 + 0.002 * rows : 0.72 + 0.002 * rows) + out / split);
+            } else {
+                const double stream = load * uses * (bn == 64 ? 0.115 + 0.0009 * rows : 0.15 + 0.0013 * rows);
+                t = 3.3 + std::max(stream, bytes / (bn == 64 ? 5.7e6 : 6.2e6) / std::min(share, 1.0)) + load * out / split;
+            }
             if (split > 1) t += 0.4 + rows / 128 * 1.2;
             if (split == 8) t += rows / 128 * 3 + (share > 1 ? 2 : 0);
             if (t < least) {
@@ -557,19 +715,58 @@ ScaledCut scaled_cut(const ScaledParams &s, int sms) {
     return best;
 }
 
-}   // namespace
-
-cudaError_t f8_scaled_tc_launch(const ScaledParams &s, bool x_signed, int *status_word, cudaStream_t st) {
-    if (((uintptr_t)s.x | (uintptr_t)s.w) & 15) return cudaErrorNotSupported;
-    if ((s.n > 1 && (s.ldx & 15)) || (s.out > 1 && (s.ldw & 15))) return cudaErrorNotSupported;
+cudaError_t launch_scaled(const ScaledParams &s, bool x_signed, int *status_word, cudaStream_t st) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     const int sms = sm_count(dev);
     if (!status_word || sms <= 0) return cudaErrorMemoryAllocation;
-    const ScaledCut cut = scaled_cut(s, sms);
-    if (cut.bn == 256) return launch_pairs(s, x_signed, status_word, dev, st);
-    if (cut.bn == 128) return launch_split<128>(s, x_signed, cut.split, status_word, dev, st);
-    return launch_split<64>(s, x_signed, cut.split, status_word, dev, st);
+    // blocks of a launch: beyond this neither matrix would fit the device's memory
+    if (((long long)s.n + 127) / 128 * (((long long)s.out + 63) / 64) * 8 > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    const bool soft = (((uintptr_t)s.x | (uintptr_t)s.w) & 15) || (s.n > 1 && (s.ldx & 15)) || (s.out > 1 && (s.ldw & 15));
+    if (!soft) {
+        const ScaledCut cut = scaled_cut(s, sms, false);
+        e = cut.bn == 256   ? launch_pairs(s, x_signed, status_word, dev, st)
+            : cut.bn == 128 ? launch_split<128, false>(s, x_signed, cut.split, status_word, dev, st)
+                            : launch_split<64, false>(s, x_signed, cut.split, status_word, dev, st);
+        if (e != cudaErrorNotSupported) return e;       // a matrix no tensor map describes: by the warps
+    }
+    const ScaledCut cut = scaled_cut(s, sms, true);
+    if (cut.bn == 128) return launch_split<128, true>(s, x_signed, cut.split, status_word, dev, st);
+    return launch_split<64, true>(s, x_signed, cut.split, status_word, dev, st);
+}
+
+}   // namespace
+
+extern "C" f8_status f8_linear_scaled(const f8_scaled_desc *desc, const void *x, const float *x_scale, const int8_t *w, const float *w_scale,
+                                      const void *bias, void *y, void *cuda_stream) {
+    if (!desc) return f8_set_error(F8_ERR_NULL, "descriptor is NULL");
+    f8_scaled_desc d = *desc;
+    if (d.n < 0 || d.k <= 0 || d.out <= 0 || d.n > 0x7fffff00 || d.out > 0x7fffff00)
+        return f8_set_error(F8_ERR_SHAPE, "n >= 0, k > 0 and out > 0 are needed, n and out at most 2^31 - 256");
+    if (d.x_dtype != F8_U8 && d.x_dtype != F8_S8) return f8_set_error(F8_ERR_DTYPE, "x_dtype must be F8_U8 or F8_S8");
+    const int ys = real_size(d.y_dtype), bs = bias ? real_size(d.bias_dtype) : 1;
+    if (!ys || !bs) return f8_set_error(F8_ERR_DTYPE, "y_dtype and bias_dtype must be F8_F32, F8_F16 or F8_BF16");
+    if ((long long)d.k * (d.x_dtype == F8_U8 ? 255 : 128) * 128 >= (1ll << 31))
+        return f8_set_error(F8_ERR_ACC_BOUND, "k products cannot be guaranteed to fit the int32 accumulator");
+    if ((d.x_scales != 1 && d.x_scales != d.n) || (d.w_scales != 1 && d.w_scales != d.out))
+        return f8_set_error(F8_ERR_SHAPE, "x_scales must be n or 1, w_scales out or 1");
+    if (d.ldx == 0) d.ldx = d.k;
+    if (d.ldw == 0) d.ldw = d.k;
+    if (d.ldy == 0) d.ldy = d.out;
+    const long long most = 1ll << 40;
+    if (d.ldx < d.k || d.ldw < d.k || d.ldy < d.out || d.ldx > most || d.ldw > most || d.ldy > most ||
+        (d.n > 1 && (d.ldx > (1ll << 50) / d.n || d.ldy > (1ll << 50) / d.n)) || d.ldw > (1ll << 50) / d.out)
+        return f8_set_error(F8_ERR_SHAPE, "a row distance is smaller than the row, or too large");
+    if (d.n == 0) return F8_OK;
+    if (!x || !x_scale || !w || !w_scale || !y) return f8_set_error(F8_ERR_NULL, "x, w, their scales and y must not be NULL");
+    if ((((uintptr_t)x_scale | (uintptr_t)w_scale) & 3) || ((uintptr_t)y & (uintptr_t)(ys - 1)) || ((uintptr_t)bias & (uintptr_t)(bs - 1)))
+        return f8_set_error(F8_ERR_ALIGN, "a pointer is not aligned to its element");
+    if (f8_pending_timeout() != F8_OK) return F8_ERR_TIMEOUT;
+    const ScaledParams p = {d.n, d.k, d.out, d.y_dtype, d.bias_dtype, d.x_scales, d.w_scales, d.ldx, d.ldw, d.ldy, (const uint8_t *)x,
+                            (const uint8_t *)w, x_scale, w_scale, bias, y};
+    const cudaError_t e = launch_scaled(p, d.x_dtype == F8_S8, f8_status_word(), (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return f8_set_error(F8_ERR_CUDA, cudaGetErrorString(e));
+    return F8_OK;
 }
