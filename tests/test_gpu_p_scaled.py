@@ -193,6 +193,65 @@ def test_same_result_every_time():
         assert all(torch.equal(y, ys[0]) for y in ys[1:])
 
 
+@pytest.mark.parametrize("n,k,out,ldw", [(2, 96, 3, 2_400_000_000), (2, 97, 3, 2_400_000_001), (300, 4096, 3, 2_400_000_000)])
+def test_rows_beyond_four_gigabytes(n, k, out, ldw):
+    """Rows of weights and of outputs whose distance from the first passes 32 bits."""
+    a = api()
+    rng = np.random.default_rng(k)
+    flat = torch.zeros(2 * ldw + k + 64, dtype=torch.int8, device="cuda")
+    w = torch.as_strided(flat, (out, k), (ldw, 1))
+    w.copy_(_codes(rng, out, k, torch.int8))
+    x = _codes(rng, n, k, torch.int8).cuda()
+    xs, ws = torch.rand(n, device="cuda"), torch.rand(out, device="cuda")
+    ldy = 3_000_000_000 if n == 2 else 20_000_000
+    y = torch.as_strided(torch.zeros((n - 1) * ldy + out, dtype=BF16, device="cuda"), (n, out), (ldy, 1))
+    a.f8_linear_scaled(x, xs, w, ws, y)
+    torch.cuda.synchronize()
+    a.f8_device_status()
+    _check(y, x, xs, w, ws, None)
+
+
+def test_many_rows_of_weights():
+    """More than four gigabytes of weights, one token."""
+    a = api()
+    out, k = 600_000, 8192
+    w = torch.zeros(out, k, dtype=torch.int8, device="cuda")
+    w[-5:] = torch.randint(-127, 128, (5, k), dtype=torch.int8, device="cuda")
+    x = torch.randint(-127, 128, (1, k), dtype=torch.int8, device="cuda")
+    one, y = torch.full((1,), 0.01, device="cuda"), torch.full((1, out), 9.0, device="cuda")
+    a.f8_linear_scaled(x, one, w, one, y)
+    torch.cuda.synchronize()
+    _check(y[:, -5:], x, one, w[-5:], one, None)
+    assert not bool(y[:, :-5].any())
+
+
+def test_a_pending_record_of_a_timeout_is_reported():
+    """Every entry point looks at the record of a wait that ran out before it enqueues anything, and works again once it is cleared."""
+    a = api()
+    x, w, y = torch.ones(2, 64, dtype=torch.int8, device="cuda"), torch.ones(8, 64, dtype=torch.int8, device="cuda"), torch.zeros(2, 8, device="cuda")
+    one, r = torch.ones(1, device="cuda"), torch.ones(2, 64, device="cuda")
+    q, s, h = torch.zeros(2, 64, dtype=torch.int8, device="cuda"), torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    calls = [lambda: a.f8_linear_scaled(x, one, w, one, y), lambda: a.f8_quantize_rows(r, q, s), lambda: a.f8_norm_quantize(r, q, s), lambda: a.f8_token_logprobs(r, entropy=h)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    y.zero_()
+    a.f8_debug_wait_timeout_probe(1.0)
+    torch.cuda.synchronize()
+    for call in calls:
+        with pytest.raises(a.F8Error) as e:
+            call()
+        assert e.value.status == 11
+    with pytest.raises(a.F8Error):
+        a.f8_device_status()
+    assert not bool(y.any())
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    a.f8_device_status()
+    assert bool((y == 64).all())
+
+
 def test_no_rows_is_a_noop():
     a = api()
     one = torch.ones(1, device="cuda")

@@ -267,6 +267,35 @@ def test_rows_captured_and_replayed():
     same_codes(so.float(), q2, s2)
 
 
+@pytest.mark.parametrize("ld,c", [(2_300_000_000, 4096), (2_300_000_001, 515), (1_200_000_000, 20001)])
+def test_rows_beyond_four_gigabytes(ld, c):
+    """Rows whose distance passes 32 bits, in bytes and in elements: the last row of each tensor is the one looked at."""
+    a = api()
+    flat = torch.zeros(2 * ld + c + 64, dtype=BF16, device="cuda")
+    x = torch.as_strided(flat, (3, c), (ld, 1))
+    x[2] = torch.randn(c, device="cuda")
+    q, s, y = torch.empty(3, c, dtype=torch.int8, device="cuda"), torch.empty(3, device="cuda"), torch.empty(3, c, dtype=BF16, device="cuda")
+    a.f8_quantize_rows(x, q, s, y=y)
+    same_codes(x.float(), q, s, y)
+    keep = x.float()
+    a.f8_norm_quantize(x, None, None, y, residual=x, residual_out=x, pre_norm=a.F8_NORM_NONE)
+    assert torch.equal(x.float(), 2 * keep) and torch.equal(y.float(), 2 * keep)
+
+
+def test_many_rows_beyond_four_gigabytes():
+    a = api()
+    n, c = 600_000, 4096
+    x = torch.zeros(n, c, dtype=BF16, device="cuda")
+    x[-3:] = torch.randn(3, c, device="cuda")
+    q, s = torch.full((n, c), 5, dtype=torch.int8, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    a.f8_quantize_rows(x, q, s)
+    same_codes(x[-3:].float(), q[-3:], s[-3:])
+    assert not bool(s[:-3].any()) and not bool(q[:-3].any())
+    out = torch.empty_like(x)
+    a.f8_norm_quantize(x, q, s, residual=x, residual_out=out, pre_norm=a.F8_NORM_NONE)
+    assert torch.equal(out[-3:].float(), 2 * x[-3:].float()) and not bool(out[:-3].any())
+
+
 def test_no_rows():
     a = api()
     x = torch.zeros(0, 64, device="cuda")

@@ -182,6 +182,34 @@ def test_strided_and_unaligned_rows(t, pad, offset):
         _run(x, tokens=2, top=min(20, v), fl=12)
 
 
+@pytest.mark.parametrize("n,v,top", [(300, 262144, 20), (1, 400000, 32)])
+def test_large_logits_that_one_thread_meets(n, v, top):
+    """Large logits at one place of every stretch that the threads of a block share out, more of them than candidates are kept."""
+    logits = torch.zeros(n, v, device="cuda")
+    logits[0] = torch.randn(v, device="cuda") * 0.1
+    for k in range(4):
+        logits[0, 20 + k::1024] = 5 + torch.rand(logits[0, 20 + k::1024].shape[0], device="cuda")
+    logits[n - 1, 20::1024] = 7
+    logits[n - 1, 21::1024] = 7
+    logits[n - 1, 22::1024] = 7
+    logits[n - 1, 23::1024] = 7
+    _run(logits, tokens=1, top=top)
+
+
+def test_rows_beyond_four_gigabytes():
+    """Rows whose distance from the first passes 32 bits, in bytes and in elements."""
+    a = api()
+    n, v = 2, 60001
+    flat = torch.zeros(4_500_000_000 + v + 64, dtype=BF16, device="cuda")
+    logits = torch.as_strided(flat, (n, v), (4_500_000_000, 1))
+    logits[1] = torch.randn(v, device="cuda") * 3
+    h, ti = torch.empty(n, device="cuda"), torch.empty(n, 4, dtype=torch.int64, device="cuda")
+    a.f8_token_logprobs(logits, entropy=h, top_ids=ti)
+    order = torch.sort(logits[1].float(), descending=True, stable=True).indices[:4]
+    assert torch.equal(ti[1], order) and ti[0].tolist() == [0, 1, 2, 3]
+    assert abs(float(h[0]) - float(torch.log(torch.tensor(v, dtype=torch.float64)))) < 1e-4
+
+
 def test_single_outputs_and_no_rows():
     a = api()
     logits = torch.randn(7, 500, device="cuda").to(BF16)
