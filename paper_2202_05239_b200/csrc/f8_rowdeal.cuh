@@ -100,7 +100,7 @@ struct Deal {
     static constexpr int VEC = 16 / sizeof(T), PER = E / VEC, PAIRS = VEC / 2;
     int c, first;
     __device__ __forceinline__ Deal(const void *row, int c_) : c(c_) {
-        const int tid = (int)(threadIdx.x & (THREADS - 1));
+        const int tid = (int)(THREADS == 32 ? threadIdx.x & 31 : threadIdx.x);
         const int m = MODE == SHIFT ? (int)((uintptr_t)row / sizeof(T) % VEC) : 0;
         first = MODE == LOOSE ? tid : tid * VEC - m;
     }

@@ -139,6 +139,7 @@ cudaError_t launch_row_quantize(const RowsParams &p, long long n, cudaStream_t s
     if (need <= 32 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 32>(p, n, st);
     if (need <= 64 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 64>(p, n, st);
     if (need <= 128 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 128>(p, n, st);
+    if (need <= 160 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 160>(p, n, st);      // (just over 2048: a row of odd width, shifted)
     if (need <= 256 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 256>(p, n, st);
     if (need <= 512 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 512>(p, n, st);
     return launch_row_quantize_at<T, ACT, MODE, 1024>(p, n, st);

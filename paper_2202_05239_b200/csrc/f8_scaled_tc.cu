@@ -451,16 +451,28 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) scaled_pair_kernel(const __gr
         const int quad = warp & 3, half = (warp - 4) >> 2, t256 = (int)threadIdx.x - 128;
         const int size = p.s.y_dtype == F8_F32 ? 4 : 2;
         int local = 0;
+        // a tile's scales and bias come while the tile before it leaves
+        float next_w = 0.f, next_b = 0.f, next_x = 0.f;
+        auto prefetch = [&](int t) {
+            if (t >= tiles) return;
+            int m_t, n_t;
+            pair_tile(t, p, m_t, n_t);
+            const int o = 256 * n_t + t256, m = 256 * m_t + 128 * rank + 32 * quad + lane;
+            next_w = o < p.s.out ? p.s.ws[p.s.w_scales == 1 ? 0 : o] : 0.f;
+            next_b = p.s.bias && o < p.s.out ? load_real(p.s.bias, p.s.bias_dtype, o) : 0.f;
+            next_x = m < p.s.n ? p.s.xs[p.s.x_scales == 1 ? 0 : m] : 0.f;
+        };
+        prefetch(worker);
         for (int t = worker; t < tiles; t += workers, ++local) {
             int m_t, n_t;
             pair_tile(t, p, m_t, n_t);
             const int acc = local & 1, n0 = 256 * n_t, m = 256 * m_t + 128 * rank + 32 * quad + lane;
             float *const f = factors + 512 * acc;
-            const bool col = n0 + t256 < p.s.out;
-            f[t256] = col ? p.s.ws[p.s.w_scales == 1 ? 0 : n0 + t256] : 0.f;
-            f[256 + t256] = col && p.s.bias ? load_real(p.s.bias, p.s.bias_dtype, n0 + t256) : 0.f;
-            const float sx = m < p.s.n ? p.s.xs[p.s.x_scales == 1 ? 0 : m] : 0.f;
+            f[t256] = next_w;
+            f[256 + t256] = next_b;
+            const float sx = next_x;
             asm volatile("bar.sync 1, 256;" ::: "memory");
+            prefetch(t + workers);
             if (!warp_wait(tfull + 8 * acc, (local >> 1) & 1, wc, 163)) continue;      // (the others may wait at the barrier above)
             tc_fence_after();
             const uint32_t from = tmem + ((uint32_t)(32 * quad) << 16) + 256u * acc + 128u * half;
