@@ -1,6 +1,8 @@
-// f8_linear_scaled on the fifth-generation tensor cores (tcgen05.mma kind::i8, int32 accumulators in tensor memory).
+// f8_linear_scaled, from two rows on with the fifth-generation tensor cores (tcgen05.mma kind::i8, int32 accumulators in tensor memory).
 //
 //     y[i, j] = round( fma((float)acc * sx[i], sw[j], b[j]) ),   acc = sum_k x[i, k] w[j, k]
+//
+// scaled_token_kernel: one row of x, on the CUDA cores (below).
 //
 // scaled_split_kernel: products whose weights are read once or a few times (decoding batches, narrow layers).  A tile is 128 rows of x
 // (as many as there are) by BN rows of w, its K divided among up to eight blocks of a cluster, so that all SMs fetch weights however
@@ -329,6 +331,57 @@ __global__ void __launch_bounds__(SPLIT_THREADS + (SOFT ? SOFT_THREADS : 0), 1) 
     }
     __syncwarp();
     if (p.split > 1) cluster_sync_all();       // no block goes while another may read it
+}
+
+// ----------------------------------------------------------------------------- one row of x
+
+// The product of one token is bound by reading the weights once and, up to some tens of megabytes, by the chain of one launch: here a row of
+// w a warp, straight from memory into dot products of four bytes (dp4a), four loads of 16 bytes a lane on their way and as many of
+// x out of the first-level cache, one integer reduction over the warp.  No shared memory, no barrier, nothing to set up.
+// 4096 x 4096: 5.1 us (split kernel 6.7), 1024 x 8192: 3.6 (4.5), 8192 x 28672: 36.5, 6.4 TB/s (38.6).  Two rows a warp 5.6 / 3.1 / 37.6, eight
+// loads 7.5 / 5.2 / 39.7; two tokens in this form 8.2 at 4096 x 4096 (split kernel 6.8).
+constexpr int TOKEN_THREADS = 128, TOKEN_UNROLL = 4;
+
+template <bool SIGNED>
+__device__ __forceinline__ int dot4(uint32_t x, uint32_t w, int acc) {
+    int d;
+    if (SIGNED) asm("dp4a.s32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(w), "r"(acc));
+    else asm("dp4a.u32.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(x), "r"(w), "r"(acc));
+    return d;
+}
+
+template <bool SIGNED>
+__global__ void __launch_bounds__(TOKEN_THREADS) scaled_token_kernel(ScaledParams p) {
+    wait_for_stream();
+    let_stream_go_on();
+    const int lane = threadIdx.x & 31;
+    const long long o = (long long)blockIdx.x * (TOKEN_THREADS / 32) + (threadIdx.x >> 5);
+    if (o >= p.out) return;
+    const uint8_t *const w = p.w + o * p.ldw;
+    const float sx = p.xs[0], sw = p.ws[p.w_scales == 1 ? 0 : o], b = p.bias ? load_real(p.bias, p.bias_dtype, o) : 0.f;
+    int acc = 0;
+    const int vectors = (p.k + 15) / 16;        // (the last one may be part of a vector: its bytes of x are made zeros)
+    for (int v0 = lane; v0 < vectors; v0 += 32 * TOKEN_UNROLL) {
+        uint4 wv[TOKEN_UNROLL], xv[TOKEN_UNROLL];
+#pragma unroll
+        for (int u = 0; u < TOKEN_UNROLL; ++u) {
+            const int v = v0 + 32 * u;
+            wv[u] = xv[u] = make_uint4(0, 0, 0, 0);
+            if (v < vectors) {
+                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(wv[u].x), "=r"(wv[u].y), "=r"(wv[u].z), "=r"(wv[u].w)
+                             : "l"(w + 16ll * v)
+                             : "memory");
+                xv[u] = *(const uint4 *)(p.x + 16ll * v);
+                if (16 * v + 16 > p.k) xv[u] = first_bytes(xv[u], p.k - 16 * v);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < TOKEN_UNROLL; ++u)
+            acc = dot4<SIGNED>(xv[u].w, wv[u].w, dot4<SIGNED>(xv[u].z, wv[u].z, dot4<SIGNED>(xv[u].y, wv[u].y, dot4<SIGNED>(xv[u].x, wv[u].x, acc))));
+    }
+    acc = __reduce_add_sync(0xffffffffu, acc);
+    if (lane == 0) store_real(p.y, p.y_dtype, o, scaled(acc, sx, sw, b));
 }
 
 // ----------------------------------------------------------------------------- pairs of blocks, 256 x 256 tiles
@@ -737,6 +790,11 @@ cudaError_t launch_scaled(const ScaledParams &s, bool x_signed, int *status_word
     // blocks of a launch: beyond this neither matrix would fit the device's memory
     if (((long long)s.n + 127) / 128 * (((long long)s.out + 63) / 64) * 8 > 0x7fffffffll) return cudaErrorInvalidConfiguration;
     const bool soft = (((uintptr_t)s.x | (uintptr_t)s.w) & 15) || (s.n > 1 && (s.ldx & 15)) || (s.out > 1 && (s.ldw & 15));
+    // One token: a warp a row of w.  Few long rows leave it without enough loads on their way: 16384 x 256 8.5 us, split kernel 6.1.
+    if (!soft && s.n == 1 && (s.k <= 4096 || s.out >= 4096)) {
+        const dim3 grid((unsigned)(((long long)s.out + TOKEN_THREADS / 32 - 1) / (TOKEN_THREADS / 32)));
+        return x_signed ? launch_early(scaled_token_kernel<true>, grid, TOKEN_THREADS, 0, st, s) : launch_early(scaled_token_kernel<false>, grid, TOKEN_THREADS, 0, st, s);
+    }
     if (!soft) {
         const ScaledCut cut = scaled_cut(s, sms, false);
         e = cut.bn == 256   ? launch_pairs(s, x_signed, status_word, dev, st)
