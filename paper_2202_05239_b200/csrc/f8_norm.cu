@@ -101,51 +101,86 @@ __global__ void __launch_bounds__(ROW_THREADS) long_norm_kernel(NormParams p) {
 }
 
 
-// One value of the threads of a row.  Every warp writes its part to its own word of `room`, which no other reduction uses within two barriers.
-template <int THREADS, typename V, typename Op>
-__device__ __forceinline__ V row_gather(Op op, const V *room) {
+// Sums over R rows (one or two) that the threads of a block hold, each thread a part of every row.  Every warp writes its part to its own
+// word of `room`, which no other reduction uses within two barriers.  Two rows share the steps: half of a warp's lanes add up one row, half the
+// other.
+template <int THREADS, int R>
+__device__ __forceinline__ void row_sums(float (&v)[R], float (*room)[32]) {
     constexpr int WARPS = THREADS / 32;
-    V v = room[threadIdx.x & (WARPS - 1)];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (R == 1) {
+        v[0] = warp_reduce(v[0], SumOp());
+        if (THREADS == 32) return;
+        if (lane == 0) room[0][warp] = v[0];
+        __syncthreads();
+        v[0] = room[0][lane & (WARPS - 1)];
 #pragma unroll
-    for (int d = WARPS / 2; d > 0; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
+        for (int d = WARPS / 2; d > 0; d >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+    } else {
+        const bool second = lane & 16;
+        float w = (second ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, second ? v[0] : v[1], 16);
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
+        if (THREADS != 32) {
+            if ((lane & 15) == 0) room[second][warp] = w;
+            __syncthreads();
+            const float *const part = room[second];
+            w = part[lane & (WARPS >= 16 ? 15 : WARPS - 1)];
+            if (WARPS == 32) w += part[16 + (lane & 15)];
+#pragma unroll
+            for (int d = WARPS >= 16 ? 8 : WARPS / 2; d > 0; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
+        }
+        v[0] = __shfl_sync(0xffffffffu, w, 0);
+        v[1] = __shfl_sync(0xffffffffu, w, 16);
+    }
 }
-template <int THREADS>
-__device__ __forceinline__ float row_sum(float v, float *room) {
-    v = warp_reduce(v, SumOp());
-    if (THREADS == 32) return v;
-    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return row_gather<THREADS>(SumOp(), room);
+// The same with the largest of a magnitude each beside the sums (sum: whether there are sums).
+template <int THREADS, int R>
+__device__ __forceinline__ void row_peaks(uint32_t (&top)[R], uint32_t (*room)[32], bool wait) {
+    constexpr int WARPS = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (!wait) {            // first half: before the barrier
+            top[r] = warp_reduce(top[r], UMaxOp());
+            if (THREADS != 32 && lane == 0) room[r][warp] = top[r];
+        } else if (THREADS != 32) {
+            top[r] = warp_reduce(room[r][lane & (WARPS - 1)], UMaxOp());
+        }
+    }
 }
 
-template <typename T, RowMode MODE, int THREADS, int E>
+template <typename T, RowMode MODE, int THREADS, int E, int R>
 __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_norm_kernel(NormParams p, bool w32, long long n) {
     wait_for_stream();
     let_stream_go_on();
     constexpr int BLOCK = row_block(THREADS), GROUPS = BLOCK / THREADS;
     extern __shared__ uint4 smem[];
-    __shared__ float rooms[2][4][32];
-    __shared__ uint32_t urooms[2][32];
+    __shared__ float rooms[2][4][R][32];
+    __shared__ uint32_t urooms[2][R][32];
     using D = Deal<T, MODE, THREADS, E>;
     constexpr int PER = D::PER, PAIRS = D::PAIRS;
     constexpr bool PIPE = MODE != LOOSE, KEEP = E == 8;       // (rows of a block lie alike: they meet the same weights)
     const float per = 1.f / (float)p.c;
     const bool own_gate = p.gate && p.ldg, fold = !p.post_b;
     const int tensors = 1 + (p.res ? 1 : 0) + (own_gate ? 1 : 0), gate_at = tensors - 1;
-    const Ring<BLOCK, PER> ring(smem, tensors);
+    const Ring<BLOCK, PER> ring(smem, R * tensors);
+    // rows row, row + step, .. of a round of R; then R * step further
     const uint32_t step = gridDim.x * GROUPS, rows = (uint32_t)n;
     uint32_t row = GROUPS == 1 ? blockIdx.x : threadIdx.x / THREADS * gridDim.x + blockIdx.x;
     const uint32_t bx = (uint32_t)p.ldx * sizeof(T), br = (uint32_t)p.ldr * sizeof(T), bg = (uint32_t)p.ldg * sizeof(T);
     const uint32_t bs = (uint32_t)p.lds * sizeof(T), by = (uint32_t)p.ldy * sizeof(T), bq = (uint32_t)p.ldq;
     const D d(row_at((const T *)p.x, row, bx), p.c);
-    auto send = [&](uint32_t r, int stage) {
-        if (r < rows) {
+    auto send = [&](uint32_t first, int stage) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t at = first + r * step;
+            if (at >= rows) continue;
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                d.send(row_at((const T *)p.x, r, bx), j, ring.place(stage, 0, j));
-                if (p.res) d.send(row_at((const T *)p.res, r, br), j, ring.place(stage, 1, j));
-                if (own_gate) d.send(row_at((const T *)p.gate, r, bg), j, ring.place(stage, gate_at, j));
+                d.send(row_at((const T *)p.x, at, bx), j, ring.place(stage, r * tensors, j));
+                if (p.res) d.send(row_at((const T *)p.res, at, br), j, ring.place(stage, r * tensors + 1, j));
+                if (own_gate) d.send(row_at((const T *)p.gate, at, bg), j, ring.place(stage, r * tensors + gate_at, j));
             }
         }
         ring_commit();
@@ -188,44 +223,64 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             f[i] = pair(gate_value(g.x, p.gate_act), gate_value(g.y, p.gate_act));
         }
     };
-    for (int stage = 0; row < rows; row += step, stage ^= 1) {
-        float (*const room)[32] = rooms[stage];
-        uint32_t *const uroom = urooms[stage];
+    for (int stage = 0; row < rows; row += R * step, stage ^= 1) {
+        float (*const room)[R][32] = rooms[stage];
+        uint32_t (*const uroom)[32] = urooms[stage];
         if (PIPE) {
-            send(row + step, stage ^ 1);
+            send(row + R * step, stage ^ 1);
             ring_wait();
         }
-        F2 v[PER][PAIRS];
+        F2 v[R][PER][PAIRS];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) unpack<T>(PIPE ? d.take(j, ring.place(stage, 0, j)) : d.load(row_at((const T *)p.x, row, bx), j), v[j]);
+        for (int r = 0; r < R; ++r)         // (a second row that is not there: what the ring held before, which nothing is written from)
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                unpack<T>(PIPE ? d.take(j, ring.place(stage, r * tensors, j)) : d.load(row_at((const T *)p.x, row, bx), j), v[r][j]);
         // v <- (v - mean) / deviation
-        auto standardize = [&](int kind, float (*rm)[32]) {
-            F2 s = 0ull;
+        auto standardize = [&](int kind, float (*rm)[R][32]) {
+            float s[R];
             if (kind == F8_NORM_LAYER) {
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    F2 t = 0ull;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) t = add2(t, v[r][j][i]);
+                    const float2 h = halves(t);
+                    s[r] = h.x + h.y;
+                }
+                row_sums<THREADS, R>(s, rm[0]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const F2 mean = both(-s[r] * per);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) v[r][j][i] = add2(v[r][j][i], mean);
+                        d.mask(j, v[r][j]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                F2 t = 0ull;
 #pragma unroll
                 for (int j = 0; j < PER; ++j)
 #pragma unroll
-                    for (int i = 0; i < PAIRS; ++i) s = add2(s, v[j][i]);
-                const float2 h = halves(s);
-                const F2 mean = both(-row_sum<THREADS>(h.x + h.y, rm[0]) * per);
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-#pragma unroll
-                    for (int i = 0; i < PAIRS; ++i) v[j][i] = add2(v[j][i], mean);
-                    d.mask(j, v[j]);
-                }
-                s = 0ull;
+                    for (int i = 0; i < PAIRS; ++i) t = fma2(v[r][j][i], v[r][j][i], t);
+                const float2 h = halves(t);
+                s[r] = h.x + h.y;
             }
+            row_sums<THREADS, R>(s, rm[1]);
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
+            for (int r = 0; r < R; ++r) {
+                const F2 rstd = both(rsqrtf(s[r] * per + p.eps));
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) s = fma2(v[j][i], v[j][i], s);
-            const float2 h = halves(s);
-            const F2 rstd = both(rsqrtf(row_sum<THREADS>(h.x + h.y, rm[1]) * per + p.eps));
+                for (int j = 0; j < PER; ++j)
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-#pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], rstd);
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], rstd);
+            }
         };
         auto by_factors = [&](bool post) {
 #pragma unroll
@@ -233,7 +288,9 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
                 F2 f[PAIRS];
                 if (!KEEP) factor(j, f, post);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], KEEP ? kept[KEEP && !post ? 1 : 0][j][i] : f[i]);
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], KEEP ? kept[KEEP && !post ? 1 : 0][j][i] : f[i]);
             }
         };
         auto plus = [&](const void *b) {
@@ -244,7 +301,9 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
                 if (sizeof(T) == 4 || w32) d.template weights<true>(b, j, f);
                 else d.template weights<sizeof(T) == 4>(b, j, f);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = add2(v[j][i], f[i]);
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = add2(v[r][j][i], f[i]);
             }
         };
         if (p.post_norm != F8_NORM_NONE) standardize(p.post_norm, room);
@@ -259,24 +318,28 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
                     d.template weights<sizeof(T) == 4>(p.gate, j, f);
                     activate_gate(f);
 #pragma unroll
-                    for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], f[i]);
                 }
             }
         }
         if (own_gate) {
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                F2 f[PAIRS];
-                unpack<T>(PIPE ? d.take(j, ring.place(stage, gate_at, j)) : d.load(row_at((const T *)p.gate, row, bg), j), f);
-                activate_gate(f);
+            for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
-            }
+                for (int j = 0; j < PER; ++j) {
+                    F2 f[PAIRS];
+                    unpack<T>(PIPE ? d.take(j, ring.place(stage, r * tensors + gate_at, j)) : d.load(row_at((const T *)p.gate, row, bg), j), f);
+                    activate_gate(f);
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], f[i]);
+                }
         }
         // the residual sum
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            F2 f[PAIRS], t[PAIRS];
+            F2 f[PAIRS];
             if (fold && KEEP) {
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[i] = kept[0][j][i];
@@ -286,50 +349,62 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
                 for (int i = 0; i < PAIRS; ++i) f[i] = both(p.branch_scale);
             }
-            if (p.res) {
-                unpack<T>(PIPE ? d.take(j, ring.place(stage, 1, j)) : d.load(row_at((const T *)p.res, row, br), j), t);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = fma2(v[j][i], f[i], t[i]);
-            } else {
+            for (int r = 0; r < R; ++r) {
+                if (p.res) {
+                    F2 t[PAIRS];
+                    unpack<T>(PIPE ? d.take(j, ring.place(stage, r * tensors + 1, j)) : d.load(row_at((const T *)p.res, row, br), j), t);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f[i]);
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = fma2(v[r][j][i], f[i], t[i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], f[i]);
+                }
+                if (p.sum && (r == 0 || row + r * step < rows)) d.store(row_at((T *)p.sum, row + r * step, bs), j, v[r][j]);
             }
-            if (p.sum) d.store(row_at((T *)p.sum, row, bs), j, v[j]);
         }
         if (!p.q && !p.y) continue;
-        float peak = 0.f;
-        uint32_t top;
-        if (p.q && p.pre_norm == F8_NORM_RMS && !p.pre_b) {
-            // the sum of squares and max |t w| in one reduction: v = (t w) * rstd, and the product with one rstd keeps the order
-            F2 s = 0ull;
+        float peak[R];
+        uint32_t top[R];
+        auto peaks = [&]() {
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
+            for (int r = 0; r < R; ++r) {
+                peak[r] = 0.f;
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) s = fma2(v[j][i], v[j][i], s);
-            by_factors(false);
+                for (int j = 0; j < PER; ++j)
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
-#pragma unroll
-                for (int i = 0; i < PAIRS; ++i) peak = peak_of(peak, v[j][i]);
-            const float2 h = halves(s);
-            float sq = warp_reduce(h.x + h.y, SumOp());
-            top = warp_reduce(magnitude(peak), UMaxOp());
-            if (THREADS != 32) {
-                if ((threadIdx.x & 31) == 0) {
-                    room[2][threadIdx.x >> 5] = sq;
-                    uroom[threadIdx.x >> 5] = top;
-                }
-                __syncthreads();
-                sq = row_gather<THREADS>(SumOp(), room[2]);
-                top = row_gather<THREADS>(UMaxOp(), uroom);
+                    for (int i = 0; i < PAIRS; ++i) peak[r] = peak_of(peak[r], v[r][j][i]);
+                top[r] = magnitude(peak[r]);
             }
-            const float rstd = rsqrtf(sq * per + p.eps);
-            top = magnitude(__uint_as_float(top) * rstd);
-            const F2 f = both(rstd);
+            row_peaks<THREADS, R>(top, uroom, false);
+        };
+        if (p.q && p.pre_norm == F8_NORM_RMS && !p.pre_b) {
+            // the sum of squares and max |t w| over one barrier: v = (t w) * rstd, and the product with one rstd keeps the order
+            float s[R];
 #pragma unroll
-            for (int j = 0; j < PER; ++j)
+            for (int r = 0; r < R; ++r) {
+                F2 t = 0ull;
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) v[j][i] = mul2(v[j][i], f);
+                for (int j = 0; j < PER; ++j)
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) t = fma2(v[r][j][i], v[r][j][i], t);
+                const float2 h = halves(t);
+                s[r] = h.x + h.y;
+            }
+            by_factors(false);
+            peaks();
+            row_sums<THREADS, R>(s, room[2]);
+            row_peaks<THREADS, R>(top, uroom, true);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float rstd = rsqrtf(s[r] * per + p.eps);
+                top[r] = magnitude(__uint_as_float(top[r]) * rstd);
+                const F2 f = both(rstd);
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], f);
+            }
         } else {
             if (p.pre_norm != F8_NORM_NONE) {
                 standardize(p.pre_norm, room + 2);
@@ -338,23 +413,25 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             }
             if (!p.q) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) d.store(row_at((T *)p.y, row, by), j, v[j]);
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+                        if (r == 0 || row + r * step < rows) d.store(row_at((T *)p.y, row + r * step, by), j, v[r][j]);
                 continue;
             }
-#pragma unroll
-            for (int j = 0; j < PER; ++j)
-#pragma unroll
-                for (int i = 0; i < PAIRS; ++i) peak = peak_of(peak, v[j][i]);
-            top = warp_reduce(magnitude(peak), UMaxOp());
-            if (THREADS != 32) {
-                if ((threadIdx.x & 31) == 0) uroom[threadIdx.x >> 5] = top;
-                __syncthreads();
-                top = row_gather<THREADS>(UMaxOp(), uroom);
-            }
+            peaks();
+            if (THREADS != 32) __syncthreads();
+            row_peaks<THREADS, R>(top, uroom, true);
         }
-        const RowScale s = RowScale::of_warp(top);
-        if (threadIdx.x % THREADS == 0) p.scale[row] = s.scale;
-        emit<T>(d, v, s, top < 0x7f800000u, row_at(p.q, row, bq), p.y ? row_at((T *)p.y, row, by) : nullptr);
+        RowScale s[R];
+        RowScale::of_warp(top, s);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t at = row + r * step;
+            if (r > 0 && at >= rows) continue;
+            if ((THREADS == 32 ? threadIdx.x & 31 : threadIdx.x) == 0) p.scale[at] = s[r].scale;
+            emit<T>(d, v[r], s[r], top[r] < 0x7f800000u, row_at(p.q, at, bq), p.y ? row_at((T *)p.y, at, by) : nullptr);
+        }
     }
 }
 
@@ -362,9 +439,14 @@ template <typename T, RowMode MODE, int THREADS, int E>
 cudaError_t launch_row_norm_at(const NormParams &p, bool w32, long long n, cudaStream_t st) {
     constexpr int PER = E * (int)sizeof(T) / 16;
     const int tensors = 1 + (p.res ? 1 : 0) + (p.gate && p.ldg ? 1 : 0);
+    if constexpr (MODE == PLAIN && E == 8 && THREADS != 32) {
+        // two rows at once where every block has several rounds of them: what a thread pays for a row beside its elements it then pays for two
+        if (n >= 8ll * 148 * (1024 / THREADS) && ring_bytes(THREADS, PER, 2 * tensors) <= RING_MOST)
+            return launch_ring<row_norm_kernel<T, MODE, THREADS, E, 2>>(THREADS, PER, 2 * tensors, n, st, p, w32);
+    }
     if (MODE != LOOSE && ring_bytes(THREADS, PER, tensors) <= RING_MOST)
-        return launch_ring<row_norm_kernel<T, MODE, THREADS, E>>(THREADS, PER, tensors, n, st, p, w32);
-    return launch_ring<row_norm_kernel<T, LOOSE, THREADS, E>>(THREADS, PER, 0, n, st, p, w32);
+        return launch_ring<row_norm_kernel<T, MODE, THREADS, E, 1>>(THREADS, PER, tensors, n, st, p, w32);
+    return launch_ring<row_norm_kernel<T, LOOSE, THREADS, E, 1>>(THREADS, PER, 0, n, st, p, w32);
 }
 template <typename T, RowMode MODE>
 cudaError_t launch_row_norm(const NormParams &p, bool w32, long long n, cudaStream_t st) {

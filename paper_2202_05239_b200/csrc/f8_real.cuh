@@ -71,17 +71,20 @@ struct RowScale {
         scale = zeros ? 0.f : __fdiv_rn(a, 127.f);
         inverse = zeros || !finite ? 0.f : __fdiv_rn(127.f, a);
     }
-    // The same for a whole warp that holds one peak: one division, by the even lanes of the first quotient, by the odd ones of the second.
-    static __device__ __forceinline__ RowScale of_warp(uint32_t peak) {
-        const float a = __uint_as_float(peak);
+    // The same for a whole warp that holds the peaks of one or two rows: one division, each quotient by lanes of its own.
+    template <int R>
+    static __device__ __forceinline__ void of_warp(const uint32_t (&peak)[R], RowScale (&s)[R]) {
+        const float a = __uint_as_float(R == 2 && (threadIdx.x & 2) ? peak[R - 1] : peak[0]);
         const bool odd = threadIdx.x & 1;
         const float q = __fdiv_rn(odd ? 127.f : a, odd ? a : 127.f);
-        RowScale s;
-        s.scale = __shfl_sync(0xffffffffu, q, 0);
-        s.inverse = __shfl_sync(0xffffffffu, q, 1);
-        if (a < 0x1p-100f) s.scale = 0.f;
-        if (a < 0x1p-100f || peak >= 0x7f800000u) s.inverse = 0.f;
-        return s;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool zeros = peak[r] < __float_as_uint(0x1p-100f);
+            s[r].scale = __shfl_sync(0xffffffffu, q, 2 * r);
+            s[r].inverse = __shfl_sync(0xffffffffu, q, 2 * r + 1);
+            if (zeros) s[r].scale = 0.f;
+            if (zeros || peak[r] >= 0x7f800000u) s[r].inverse = 0.f;
+        }
     }
     __device__ __forceinline__ RowScale() {}
     // floor(v * inverse + 1/2): the sum is rounded towards -infinity, which no integer lies under, so the floor is that of the exact

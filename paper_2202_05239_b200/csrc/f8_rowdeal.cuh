@@ -279,7 +279,7 @@ struct RowLayout {
 
 // As many blocks as the SMs hold at once, or as there are rows.  `tensors`: those whose rows go through the ring (0: none do).
 // What the runtime says of a kernel is asked once for each device and size of the ring.
-struct RingFit { std::atomic<int> held[64][4]; };
+struct RingFit { std::atomic<int> held[64][8]; };
 constexpr size_t RING_MOST = 220 * 1024;
 inline size_t ring_bytes(int threads, int per, int tensors) { return (size_t)2 * tensors * per * row_block(threads) * 16; }
 
@@ -296,7 +296,7 @@ cudaError_t launch_ring(int threads, int per, int tensors, long long n, cudaStre
     int held = fit.held[dev][tensors].load(std::memory_order_relaxed);
     if (held == 0) {
         int sms = 0, blocks = 0;
-        const size_t most = std::min(ring_bytes(threads, per, 3), RING_MOST);
+        const size_t most = RING_MOST;
         e = cudaFuncSetAttribute((const void *)KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
         if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, (const void *)KERNEL, block, smem);

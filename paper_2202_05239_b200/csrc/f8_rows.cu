@@ -118,10 +118,12 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_q
             for (int j = 0; j < PER; ++j) d.store(y, j, v[j]);
             continue;
         }
-        const uint32_t top = block_reduce<THREADS>(magnitude(peak), UMaxOp(), room[stage]);
-        const RowScale s = RowScale::of_warp(top);
+        const uint32_t top[1] = {block_reduce<THREADS>(magnitude(peak), UMaxOp(), room[stage])};
+        RowScale scales[1];
+        RowScale::of_warp(top, scales);
+        const RowScale &s = scales[0];
         if ((THREADS == 32 ? threadIdx.x & 31 : threadIdx.x) == 0) p.scale[row] = s.scale;
-        emit<T>(d, v, s, top < 0x7f800000u, row_at(p.q, row, bq), y);
+        emit<T>(d, v, s, top[0] < 0x7f800000u, row_at(p.q, row, bq), y);
     }
 }
 
