@@ -5,9 +5,11 @@
 // Bound by memory traffic: x, r (and a gate per token) are read once, t, q and the values written once; what a row needs besides is two to
 // five sums over it.  Rows of up to 16384 elements stay in registers, a warp to 32 warps a row, while the next row is on its way.  A
 // block walks many rows, and up to 8192 elements each thread keeps the factors of its 8 elements (norm weights, the post norm's already
-// multiplied by beta and a gate that all rows share).  4096 x 8192 bf16, norms on both sides, channel gate: 68 us; with 32 elements a
-// thread and the weights read again for every row 73 us (half of them came from the second-level cache), with 16 elements, several
-// rows a block and the factors in shared memory 72 us.
+// multiplied by beta and a gate that all rows share).  With rows to spare it takes two at once, which share sums, barriers and
+// the division of the scales; what bounds it then is memory, 33 instructions an element behind it.
+// 4096 x 8192 bf16, norms on both sides, channel gate, all outputs: 55 us, 5.5 TB/s.  On the way there: 32 elements a thread and the weights
+// read again for every row 73 us (half of them came from the second-level cache); 16 elements, several rows a block and the
+// factors in shared memory 72; 8 elements, one row at a time 64; two rows with the options of the call tested for each 58.
 // Longer rows take a kernel that reads the row again for every sum, from the caches.
 #include "f8_rowdeal.cuh"
 
@@ -162,8 +164,12 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
     constexpr int PER = D::PER, PAIRS = D::PAIRS;
     constexpr bool PIPE = MODE != LOOSE, KEEP = E == 8;       // (rows of a block lie alike: they meet the same weights)
     const float per = 1.f / (float)p.c;
-    const bool own_gate = p.gate && p.ldg, fold = !p.post_b;
-    const int tensors = 1 + (p.res ? 1 : 0) + (own_gate ? 1 : 0), gate_at = tensors - 1;
+    // Two rows at once only between blocks as most models have them, whose options the compiler then knows: a residual sum that is kept, no gate
+    // per token, RMS norms without biases, codes.
+    constexpr bool COMMON = R == 2;
+    const bool own_gate = !COMMON && p.gate && p.ldg, fold = COMMON || !p.post_b, has_res = COMMON || p.res, has_sum = COMMON || p.sum, has_q = COMMON || p.q;
+    const int post_norm = COMMON && p.post_norm != F8_NORM_NONE ? (int)F8_NORM_RMS : p.post_norm;
+    const int tensors = 1 + (has_res ? 1 : 0) + (own_gate ? 1 : 0), gate_at = tensors - 1;
     const Ring<BLOCK, PER> ring(smem, R * tensors);
     // rows row, row + step, .. of a round of R; then R * step further
     const uint32_t step = gridDim.x * GROUPS, rows = (uint32_t)n;
@@ -179,7 +185,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
                 d.send(row_at((const T *)p.x, at, bx), j, ring.place(stage, r * tensors, j));
-                if (p.res) d.send(row_at((const T *)p.res, at, br), j, ring.place(stage, r * tensors + 1, j));
+                if (has_res) d.send(row_at((const T *)p.res, at, br), j, ring.place(stage, r * tensors + 1, j));
                 if (own_gate) d.send(row_at((const T *)p.gate, at, bg), j, ring.place(stage, r * tensors + gate_at, j));
             }
         }
@@ -306,7 +312,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
                     for (int i = 0; i < PAIRS; ++i) v[r][j][i] = add2(v[r][j][i], f[i]);
             }
         };
-        if (p.post_norm != F8_NORM_NONE) standardize(p.post_norm, room);
+        if (post_norm != F8_NORM_NONE) standardize(post_norm, room);
         if (!fold) {
             by_factors(true);
             plus(p.post_b);
@@ -351,7 +357,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                if (p.res) {
+                if (has_res) {
                     F2 t[PAIRS];
                     unpack<T>(PIPE ? d.take(j, ring.place(stage, r * tensors + 1, j)) : d.load(row_at((const T *)p.res, row, br), j), t);
 #pragma unroll
@@ -360,10 +366,10 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
 #pragma unroll
                     for (int i = 0; i < PAIRS; ++i) v[r][j][i] = mul2(v[r][j][i], f[i]);
                 }
-                if (p.sum && (r == 0 || row + r * step < rows)) d.store(row_at((T *)p.sum, row + r * step, bs), j, v[r][j]);
+                if (has_sum && (r == 0 || row + r * step < rows)) d.store(row_at((T *)p.sum, row + r * step, bs), j, v[r][j]);
             }
         }
-        if (!p.q && !p.y) continue;
+        if (!has_q && !p.y) continue;
         float peak[R];
         uint32_t top[R];
         auto peaks = [&]() {
@@ -378,7 +384,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
             }
             row_peaks<THREADS, R>(top, uroom, false);
         };
-        if (p.q && p.pre_norm == F8_NORM_RMS && !p.pre_b) {
+        if (COMMON || (has_q && p.pre_norm == F8_NORM_RMS && !p.pre_b)) {
             // the sum of squares and max |t w| over one barrier: v = (t w) * rstd, and the product with one rstd keeps the order
             float s[R];
 #pragma unroll
@@ -411,7 +417,7 @@ __global__ void __launch_bounds__(row_block(THREADS), row_blocks(THREADS)) row_n
                 by_factors(false);
                 if (p.pre_b) plus(p.pre_b);
             }
-            if (!p.q) {
+            if (!has_q) {
 #pragma unroll
                 for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -441,7 +447,8 @@ cudaError_t launch_row_norm_at(const NormParams &p, bool w32, long long n, cudaS
     const int tensors = 1 + (p.res ? 1 : 0) + (p.gate && p.ldg ? 1 : 0);
     if constexpr (MODE == PLAIN && E == 8 && THREADS != 32) {
         // two rows at once where every block has several rounds of them: what a thread pays for a row beside its elements it then pays for two
-        if (n >= 8ll * 148 * (1024 / THREADS) && ring_bytes(THREADS, PER, 2 * tensors) <= RING_MOST)
+        const bool common = p.res && p.sum && p.q && !(p.gate && p.ldg) && p.post_norm != F8_NORM_LAYER && !p.post_b && p.pre_norm == F8_NORM_RMS && !p.pre_b;
+        if (common && n >= 8ll * 148 * (1024 / THREADS) && ring_bytes(THREADS, PER, 2 * tensors) <= RING_MOST)
             return launch_ring<row_norm_kernel<T, MODE, THREADS, E, 2>>(THREADS, PER, 2 * tensors, n, st, p, w32);
     }
     if (MODE != LOOSE && ring_bytes(THREADS, PER, tensors) <= RING_MOST)

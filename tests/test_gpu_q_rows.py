@@ -206,6 +206,39 @@ def test_step_shapes(n, c):
     _step(rng, n, c, F16, pre="layer", bias=True, gate="token")
 
 
+@pytest.mark.parametrize("n,c", [(1184, 8192), (1185, 8000), (2369, 4096), (4737, 2048), (9473, 1000), (9999, 1024), (1300, 16384)])
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+def test_step_with_many_rows(n, c, t):
+    """Several rounds of rows for every block, which then takes two rows at once between blocks with the usual options; odd numbers of rows."""
+    rng = np.random.default_rng(n)
+    _step(rng, n, c, t, post="rms", gate="channel", beta=0.5)
+    _step(rng, n, c, t, values=False, inplace=True)
+    _step(rng, n, c, t, post="rms", gate="token", gate_act="sigmoid", pre="layer", bias=True)
+
+
+@pytest.mark.parametrize("c", [2048, 8192])
+def test_rows_of_a_pair_do_not_mix(c):
+    """Rows that are not finite, zero or tiny next to ordinary ones, where two rows share their sums."""
+    a = api()
+    n = 8 * 148 * (1024 // (c // 8)) + 3
+    x, r = torch.randn(n, c, device="cuda").to(BF16), torch.randn(n, c, device="cuda").to(BF16)
+    kinds = torch.arange(n, device="cuda") % 5
+    x[kinds == 1], r[kinds == 1] = 0, 0
+    r[kinds == 2, 7] = float("nan")
+    x[kinds == 3, c - 1] = float("inf")
+    q, s, so = torch.full((n, c), 9, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(r)
+    w = torch.ones(c, device="cuda")
+    a.f8_norm_quantize(x, q, s, residual=r, residual_out=so, post_norm=a.F8_NORM_RMS, post_w=w, pre_w=w)
+    one = [i for i in range(n) if i % 5 in (0, 4)]
+    q1, s1, so1 = torch.empty(1, c, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda"), torch.empty(1, c, dtype=BF16, device="cuda")
+    assert not bool(s[kinds == 1].any()) and not bool(q[kinds == 1].any())
+    assert bool(torch.isnan(s[(kinds == 2) | (kinds == 3)]).all()) and not bool(q[(kinds == 2) | (kinds == 3)].any())
+    for i in one[:4] + one[-4:]:
+        a.f8_norm_quantize(x[i:i + 1], q1, s1, residual=r[i:i + 1], residual_out=so1, post_norm=a.F8_NORM_RMS, post_w=w, pre_w=w)
+        assert bool(((q1[0].int() - q[i].int()).abs() <= 1).all()) and abs(float(s1) - float(s[i])) <= 1e-5 * float(s1)
+        assert bool(((so1[0].float() - so[i].float()).abs() <= 2.0 ** -7 * so[i].float().abs() + 1e-6).all())
+
+
 @pytest.mark.parametrize("codes,values,total", [(True, False, True), (True, False, False), (False, True, True), (False, True, False), (False, False, True),
                                                 (True, True, False)])
 @pytest.mark.parametrize("c", [64, 1000, 4096, 20000])
