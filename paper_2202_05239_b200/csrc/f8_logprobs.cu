@@ -494,7 +494,7 @@ extern "C" f8_status f8_token_logprobs(const f8_logprobs_desc *desc, const void 
     if (!size) return f8_set_error(F8_ERR_DTYPE, "dtype must be F8_S32, F8_F32, F8_F16 or F8_BF16");
     if (d.dtype == F8_S32 && (d.fl < -8 || d.fl > 32)) return f8_set_error(F8_ERR_FL_RANGE, "fl outside [-8, 32]");
     const float c = d.dtype == F8_S32 ? ldexpf(d.inv_temperature, -d.fl) : d.inv_temperature;
-    if (!(c > 0.f) || !isfinite(c)) return f8_set_error(F8_ERR_SHAPE, "inv_temperature * 2^-fl leaves the range of 32-bit floats");
+    if (!(c > 0.f) || !isfinite(1.5f * c)) return f8_set_error(F8_ERR_SHAPE, "inv_temperature * 2^-fl leaves the range of 32-bit floats");
     if (d.ldl == 0) d.ldl = d.v;
     if (d.ldl < d.v || d.ldl > (1ll << 40) || (d.n > 1 && d.ldl > (1ll << 50) / d.n))
         return f8_set_error(F8_ERR_SHAPE, "the row distance is smaller than the row, or too large");

@@ -91,6 +91,24 @@ def test_activations_far_out():
         assert bool(((y.double() - want).abs() <= want.abs() * (10 + 2.4 * x.double().abs().clamp(max=200)) * 2.0 ** -23 + 1e-37).all()), (y, want)
 
 
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("c", [16, 20000])
+def test_activations_far_out_in_16_bits(t, c):
+    a = api()
+    big = 6e4 if t == F16 else 3e38
+    x = torch.zeros(1, c, device="cuda")
+    x[0, :14] = torch.tensor([-big, -1000.0, -200.0, -100.0, -88.5, -87.5, -60.0, -20.0, 0.0, 20.0, 88.5, 200.0, 1000.0, big])
+    x = x.to(t)
+    for act, f in ((a.F8_ACT_SILU, silu), (a.F8_ACT_GELU, gelu)):
+        y = torch.empty_like(x)
+        a.f8_quantize_rows(x, y=y, act=act)
+        v = x.double()
+        want = torch.where(v < -1000, torch.zeros_like(v), f(v))
+        assert bool(torch.isfinite(y).all())
+        err = want.abs() * ((10 + 2.4 * v.abs().clamp(max=200)) * 2.0 ** -23 + half_step(t)) + tiny(t) + 1e-36
+        assert bool(((y.double() - want).abs() <= 1.01 * err).all()), (y, want)
+
+
 @pytest.mark.parametrize("c", [8, 100, 4096, 20000])
 @pytest.mark.parametrize("t", [BF16, F32])
 def test_zero_tiny_and_not_finite_rows(c, t):

@@ -100,7 +100,7 @@ def _lp(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(n=-1), 2), (dict(v=0), 2), (dict(tokens=-1), 2), (dict(top=33), 2), (dict(top=-1), 2), (dict(v=4), 2), (dict(dtype=api.F8_U8), 3), (dict(dtype=api.F8_S32, fl=33), 4),
-    (dict(dtype=api.F8_S32, fl=-9), 4), (dict(inv_temperature=0.0), 2), (dict(inv_temperature=-1.0), 2), (dict(inv_temperature=NAN), 2), (dict(inv_temperature=INF), 2),
+    (dict(dtype=api.F8_S32, fl=-9), 4), (dict(inv_temperature=0.0), 2), (dict(inv_temperature=-1.0), 2), (dict(inv_temperature=NAN), 2), (dict(inv_temperature=INF), 2), (dict(inv_temperature=3e38), 2),
     (dict(dtype=api.F8_S32, fl=-8, inv_temperature=3e38), 2), (dict(dtype=api.F8_S32, fl=32, inv_temperature=1e-44), 2), (dict(ldl=99), 2), (dict(ldl=1 << 49), 2)])
 def test_logprobs_refuse(kw, status):
     assert api._lib.f8_token_logprobs(ctypes.byref(_lp(**kw)), A, A, A, A, A, A, None) == status, api._lib.f8_last_error()
