@@ -255,3 +255,17 @@ def test_network_classifies(ref):
     tol, _ = _bounds(want, h, logits.shape[1])
     assert bool(((lp.double() - want.gather(1, order)).abs() <= tol.gather(1, order)).all())
     net.close()
+
+
+@pytest.mark.parametrize("t", [S32, F32, F16, BF16])
+@pytest.mark.parametrize("v", [130, 250, 1000, 1031, 2045])
+def test_short_rows_with_many_alternatives(v, t):
+    """Rows that give fewer groups of threads an element than there are alternatives; equal logits; rows that start off a vector."""
+    rng = np.random.default_rng(v)
+    for top in (9, 17, 32):
+        _run(_logits(rng, 3, v, t), tokens=2, top=top, fl=12)
+        few = torch.from_numpy(rng.integers(-3, 3, size=(3, v))).to(t).cuda()
+        _run(few, tokens=2, top=top, fl=2)
+        view, _ = strided(3, v, t, 5, 3)
+        view.copy_(_logits(rng, 3, v, t))
+        _run(view, tokens=2, top=top, fl=12)
