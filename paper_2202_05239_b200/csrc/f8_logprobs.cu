@@ -30,6 +30,11 @@ constexpr int LP_THREADS = 256;
 // stages of 4 through shared memory and 3 40; 2 and 6 51; 4 and 5 41.
 constexpr int LP_UNROLL = 4;
 constexpr int LP_BLOCKS = 4;
+// Vectors that a thread of a block with a whole row keeps in registers where the row has no more, so that it is not read again for the
+// owner's elements and the alternatives.  256 rows of 1000 codes, 5 alternatives: none kept 5.7 us, two 5.2, four 5.3; 1024 x 50001 float:
+// none and two 38.3 us, four 39.8 (registers).  Clusters keep none: eight in 96 registers, two blocks an SM, took 17.7 us for 16 rows of
+// 131072 bf16 and 20 alternatives against 12.5.
+constexpr int LP_KEEP = 2;
 constexpr int LP_CANDIDATES = 1024;       // rows with more (as when one thread's elements hold most of the large ones) take the slow way
 constexpr int LP_MOST_TOP = 32;
 
@@ -168,7 +173,8 @@ __device__ __forceinline__ uint32_t in_block(const void *p, uint32_t rank) {
 __device__ __forceinline__ Key remote64(uint32_t a) { Key v; asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory"); return v; }
 __device__ __forceinline__ uint32_t remote32(uint32_t a) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory"); return v; }
 
-template <typename T, bool CLUSTER>
+// KEEP: see LP_KEEP.
+template <typename T, bool CLUSTER, int KEEP>
 __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParams p) {
     wait_for_stream();
     let_stream_go_on();
@@ -211,7 +217,10 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         }
         sum.add(x, N::safe(sum.m), cl);
     };
-    if (tid < head) meet(N::one(l + tid), tid);
+    // an element of the head or the tail
+    const int edge_at = tid < head ? tid : tid >= 32 && tid - 32 < tail ? tail_at + tid - 32 : -1;
+    const V edge = edge_at >= 0 ? N::one(l + edge_at) : N::lowest();
+    if (tid < head) meet(edge, edge_at);
     const T *vl = l + first;
     auto batch = [&](const uint4 *w, int count, int base) {
         V x[LP_UNROLL][VEC];
@@ -246,18 +255,54 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(vl + (long long)i * VEC) : "memory");
         return w;
     };
-    int i = tid;
-    uint4 w[LP_UNROLL];
-    for (; i + (LP_UNROLL - 1) * LP_THREADS < vecs; i += LP_UNROLL * LP_THREADS) {
+    const int rounds = (vecs + LP_THREADS - 1) / LP_THREADS;
+    const bool resident = KEEP && rounds <= KEEP;
+    uint4 w[KEEP ? KEEP : 1];
+    if (resident) {
 #pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u) w[u] = vector(i + u * LP_THREADS);
-        batch(w, LP_UNROLL, i);
+        for (int u = 0; u < KEEP; ++u) w[u] = tid + u * LP_THREADS < vecs ? vector(tid + u * LP_THREADS) : make_uint4(0, 0, 0, 0);
+        V top = N::lowest();
+        int which = -1;
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) {
+            if (tid + u * LP_THREADS >= vecs) continue;
+            V x[VEC];
+            N::unpack(w[u], x);
+            V most = x[0];
+#pragma unroll
+            for (int k = 1; k < VEC; ++k) most = N::larger(most, x[k]);
+            if (which < 0 || most > top) { top = most; which = u; }
+        }
+        if (which >= 0 && (!some || top > sum.m)) {
+            if (some) sum.raise(top, cl);
+            sum.m = top;
+            at = first + (tid + which * LP_THREADS) * VEC;
+            span = VEC - 1;
+            some = true;
+        }
+        const V ref = N::safe(sum.m);
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) {
+            if (tid + u * LP_THREADS >= vecs) continue;
+            V x[VEC];
+            N::unpack(w[u], x);
+#pragma unroll
+            for (int k = 0; k < VEC; k += 2) sum.add(x[k], x[k + 1], ref, cl);
+        }
+    } else {
+        int i = tid;
+        uint4 v[LP_UNROLL];
+        for (; i + (LP_UNROLL - 1) * LP_THREADS < vecs; i += LP_UNROLL * LP_THREADS) {
+#pragma unroll
+            for (int u = 0; u < LP_UNROLL; ++u) v[u] = vector(i + u * LP_THREADS);
+            batch(v, LP_UNROLL, i);
+        }
+        for (; i < vecs; i += LP_THREADS) {
+            v[0] = vector(i);
+            batch(v, 1, i);
+        }
     }
-    for (; i < vecs; i += LP_THREADS) {
-        w[0] = vector(i);
-        batch(w, 1, i);
-    }
-    if (tid >= 32 && tid - 32 < tail) meet(N::one(l + tail_at + tid - 32), tail_at + tid - 32);
+    if (edge_at >= tail_at) meet(edge, edge_at);
 
     // ---- the block's largest element and the sums without it
     const uint32_t mine = N::order(sum.m);
@@ -289,15 +334,28 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
             if (!lost) s += exp2_fast(N::minus(x, m) * cl);
         };
         if (best) {
-            for (int j = tid; j * LP_THREADS + who < vecs; j += LP_THREADS) {
-                V x[VEC];
-                N::unpack(vector(j * LP_THREADS + who), x);
-                const int index = first + (j * LP_THREADS + who) * VEC;
+            if (resident) {
+                if (tid == who) {
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) again(x[k], index + k, index == own_at);
+                    for (int u = 0; u < KEEP; ++u) {
+                        if (tid + u * LP_THREADS >= vecs) continue;
+                        V x[VEC];
+                        N::unpack(w[u], x);
+                        const int index = first + (tid + u * LP_THREADS) * VEC;
+#pragma unroll
+                        for (int k = 0; k < VEC; ++k) again(x[k], index + k, index == own_at);
+                    }
+                }
+            } else {
+                for (int j = tid; j * LP_THREADS + who < vecs; j += LP_THREADS) {
+                    V x[VEC];
+                    N::unpack(vector(j * LP_THREADS + who), x);
+                    const int index = first + (j * LP_THREADS + who) * VEC;
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) again(x[k], index + k, index == own_at);
+                }
             }
-            if (tid == who && tid < head) again(N::one(l + tid), tid, tid == own_at);
-            if (tid == who && tid >= 32 && tid - 32 < tail) again(N::one(l + tail_at + tid - 32), tail_at + tid - 32, tail_at + tid - 32 == own_at);
+            if (tid == who && edge_at >= 0) again(edge, edge_at, edge_at == own_at);
         }
         s = block_reduce<LP_THREADS>(s, SumOp(), froom[0]);
         t = block_reduce<LP_THREADS>(t, SumOp(), froom[1]);
@@ -329,9 +387,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         for (int d = 16; d > 0; d >>= 1) bound = max(bound, __shfl_xor_sync(0xffffffffu, bound, d));
         // ... and the top-th largest of their own maxima is the bound of the elements
         Key least = bound;
-        const int rounds = (vecs + LP_THREADS - 1) / LP_THREADS;
         // (a thread with a handful of vectors is read again sooner than its worth is looked into; but a short row has fewer groups than
-        // alternatives, no bound, and would rank all its elements: 2048 rows of 1000 bf16, top 20, 32 us so and 332 us)
+        // alternatives, no bound, and would rank all its elements: 2048 rows of 1000 bf16, top 20, 30 us so and 319 us)
         if (rounds > 4 || !bound) {
             if (low >= bound && low) found[atomicAdd(&counts[0], 1)] = low;
             __syncthreads();
@@ -342,25 +399,42 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
             __syncthreads();
             if (tid == 0) counts[0] = 0;
         }
-        if (some && high >= least) members[atomicAdd(&counts[1], 1)] = tid;
-        __syncthreads();
         auto offer = [&](V x, int index) {
             const Key k = make_key(N::order(x), index);
             if (k < least) return;
             const int n = atomicAdd(&counts[0], 1);
             if (n < LP_CANDIDATES) found[n] = k;
         };
-        const int who = counts[1];
-        for (int j = tid; j < who * rounds; j += LP_THREADS) {
-            const int at_vec = (j / who) * LP_THREADS + members[j % who];
-            if (at_vec >= vecs) continue;
-            V x[VEC];
-            N::unpack(vector(at_vec), x);
+        if (resident) {
+            if (some && high >= least) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) offer(x[k], first + at_vec * VEC + k);
+                for (int u = 0; u < KEEP; ++u) {
+                    if (tid + u * LP_THREADS >= vecs) continue;
+                    V x[VEC];
+                    N::unpack(w[u], x);
+                    V most = x[0];
+#pragma unroll
+                    for (int k = 1; k < VEC; ++k) most = N::larger(most, x[k]);
+                    const int index = first + (tid + u * LP_THREADS) * VEC;
+                    if (make_key(N::order(most), index) < least) continue;
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) offer(x[k], index + k);
+                }
+            }
+        } else {
+            if (some && high >= least) members[atomicAdd(&counts[1], 1)] = tid;
+            __syncthreads();
+            const int who = counts[1];
+            for (int j = tid; j < who * rounds; j += LP_THREADS) {
+                const int at_vec = (j / who) * LP_THREADS + members[j % who];
+                if (at_vec >= vecs) continue;
+                V x[VEC];
+                N::unpack(vector(at_vec), x);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) offer(x[k], first + at_vec * VEC + k);
+            }
         }
-        if (tid < head) offer(N::one(l + tid), tid);
-        if (tid >= 32 && tid - 32 < tail) offer(N::one(l + tail_at + tid - 32), tail_at + tid - 32);
+        if (edge_at >= 0) offer(edge, edge_at);
         if (tid < LP_MOST_TOP) part.top[tid] = 0;
         __syncthreads();
         const int n = counts[0];
@@ -466,7 +540,7 @@ int lp_blocks(long long n, long long row_bytes) {
 template <typename T>
 cudaError_t launch_logprobs(const LpParams &p, long long n, cudaStream_t st) {
     const int s = n <= 65535 ? lp_blocks(n, (long long)p.v * sizeof(T)) : 1;
-    if (s == 1) return launch_early(logprobs_kernel<T, false>, dim3((unsigned)n), LP_THREADS, 0, st, p);
+    if (s == 1) return launch_early(logprobs_kernel<T, false, LP_KEEP>, dim3((unsigned)n), LP_THREADS, 0, st, p);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)s, (unsigned)n);
     cfg.blockDim = dim3(LP_THREADS);
@@ -480,7 +554,7 @@ cudaError_t launch_logprobs(const LpParams &p, long long n, cudaStream_t st) {
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, true>, p);
+    return cudaLaunchKernelEx(&cfg, logprobs_kernel<T, true, 0>, p);
 }
 
 }   // namespace
