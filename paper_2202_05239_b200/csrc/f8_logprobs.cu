@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
     __shared__ float froom[2][32];
     __shared__ Key keys[LP_THREADS], found[LP_CANDIDATES];
     __shared__ int members[LP_THREADS];
-    __shared__ int counts[3];
+    __shared__ int counts[4];               // candidates; threads to read again; the owner of the largest element; threads worth a look
     __shared__ LpPart part;
     const int tid = threadIdx.x;
     const long long row = CLUSTER ? blockIdx.y : blockIdx.x;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
     const int first = head_all + v0 * VEC;                 // element at which the part's vectors start
     const int head = rank == 0 ? head_all : 0, tail = rank == ranks - 1 ? p.v - head_all - vecs_all * VEC : 0;
     const int tail_at = head_all + vecs_all * VEC;
-    if (tid < 3) counts[tid] = 0;
+    if (tid < 4) counts[tid] = 0;
 
     // ---- one pass: a thread takes every 256th vector, the first threads an element of the head or the tail
     Sums<T> sum;
@@ -390,14 +390,13 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         // (a thread with a handful of vectors is read again sooner than its worth is looked into; but a short row has fewer groups than
         // alternatives, no bound, and would rank all its elements: 2048 rows of 1000 bf16, top 20, 30 us so and 319 us)
         if (rounds > 4 || !bound) {
-            if (low >= bound && low) found[atomicAdd(&counts[0], 1)] = low;
+            // (counted in a counter of their own: one that is set to zero again between two uses needs a barrier on either side of that)
+            if (low >= bound && low) found[atomicAdd(&counts[3], 1)] = low;
             __syncthreads();
-            const int threads = counts[0];
+            const int threads = counts[3];
             if (tid < threads && above_in(found, threads, found[tid]) == p.top - 1) room[1][0] = found[tid];
-            __syncthreads();
+            __syncthreads();                                // (and the candidates below may go where the maxima were)
             least = threads >= p.top ? room[1][0] : 0;      // (fewer threads with elements than alternatives: all elements)
-            __syncthreads();
-            if (tid == 0) counts[0] = 0;
         }
         auto offer = [&](V x, int index) {
             const Key k = make_key(N::order(x), index);

@@ -1,4 +1,6 @@
 """Log probabilities, entropy and largest alternatives of logits (f8_token_logprobs) against their 64-bit forms."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -269,3 +271,43 @@ def test_short_rows_with_many_alternatives(v, t):
         view, _ = strided(3, v, t, 5, 3)
         view.copy_(_logits(rng, 3, v, t))
         _run(view, tokens=2, top=top, fl=12)
+
+
+@pytest.mark.parametrize("t", [S32, F32, BF16])
+@pytest.mark.parametrize("v", [10, 300, 600, 1000, 1216])
+def test_thousands_of_short_rows_with_many_alternatives(v, t):
+    """Every SM full of rows whose alternatives are bounded by single threads, or not at all, again and again: the same ones each time."""
+    rng = np.random.default_rng(v)
+    logits = _logits(rng, 6000, v, t)
+    view, _ = strided(6000, v, t, 1, 1)             # the same off a vector: elements in front of the first and behind the last
+    view.copy_(logits)
+    a = api()
+    order = torch.sort(logits.float() if t != S32 else logits, dim=1, descending=True, stable=True).indices
+    for top in (5, 20, 32):
+        if top > v:
+            continue
+        ti = torch.empty(6000, top, dtype=torch.int64, device="cuda")
+        for rows in (logits, view) * 10:
+            ti.fill_(-7)
+            a.f8_token_logprobs(rows, top_ids=ti, fl=12)
+            assert torch.equal(ti, order[:, :top])
+        _run(logits, tokens=2, top=top, fl=12)
+
+
+@pytest.mark.parametrize("classes,batch,top", [(10, 1, 5), (10, 300, 10), (100, 64, 32), (1000, 7, 1)])
+def test_networks_of_few_classes(classes, batch, top):
+    """`Net.classify` of a network whose last layer has few classes, its logits those of the forward pass."""
+    a = api()
+    layers = synth.make_net("mobilenetv1", 0, image=32)
+    last = layers[-1]
+    layers[-1] = dataclasses.replace(last, c_out=classes, weight=last.weight[:classes].copy(), bias=last.bias[:classes].copy())
+    net = a.Net(layers, batch)
+    x = a.to_device(synth.draw_image(batch, 5, 32, 32))
+    ids, lp = net.classify(x, top=top)
+    logits = net.forward(x).view(batch, classes)
+    order = torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(ids, order)
+    want, h, _ = _reference(logits, 2.0 ** -(layers[-1].fl_x + layers[-1].fl_w))
+    tol, _ = _bounds(want, h, classes)
+    assert bool(((lp.double() - want.gather(1, order)).abs() <= tol.gather(1, order)).all())
+    net.close()
