@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(SPLIT_THREADS + (SOFT ? SOFT_THREADS : 0), 1) 
 #pragma unroll
                     for (int q = 0; q < 4; ++q) sts128(at + 16 * q, make_uint4((uint32_t)v[4 * q], (uint32_t)v[4 * q + 1], (uint32_t)v[4 * q + 2], (uint32_t)v[4 * q + 3]));
                 }
+                __syncwarp();                   // the next load takes all lanes together, also those without a row
             }
         }
         tc_fence_before();
@@ -553,8 +554,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) scaled_pair_kernel(const __gr
                     r[4 * q + 2] = scaled(v[4 * q + 2], sx, w4.z, b4.z);
                     r[4 * q + 3] = scaled(v[4 * q + 3], sx, w4.w, b4.w);
                 }
-                if (m >= p.s.n) continue;
-                if (p.align >= 16 && o + 16 <= p.s.out) {
+                if (m >= p.s.n) {                               // a lane without a row
+                } else if (p.align >= 16 && o + 16 <= p.s.out) {
                     uint32_t w[8];
                     if (size == 4) {
 #pragma unroll
@@ -581,6 +582,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) scaled_pair_kernel(const __gr
                     for (int q = 0; q < 16; ++q)
                         if (o + q < p.s.out) store_real(p.s.y, p.s.y_dtype, (long long)m * p.s.ldy + o + q, r[q]);
                 }
+                __syncwarp();                                   // the next load, and the barrier of the next tile, take all lanes together
             }
         }
     }

@@ -286,3 +286,17 @@ def test_sequence_of_dependent_calls():
         src = y
         seen.append(float(y.float().abs().max()))
     assert torch.equal(last, y) and seen[-1] > 0
+
+
+@pytest.mark.parametrize("n", [4096 + 1, 4096 + 13, 4096 + 31, 4096 + 97, 4352 - 1])
+@pytest.mark.parametrize("out,pady,yt", [(2304, 0, BF16), (2301, 0, BF16), (2049, 3, F32)])
+def test_last_rows_that_fill_part_of_a_warp(n, out, pady, yt):
+    """Many tiles for each pair of blocks, rows of the last ones that only some lanes of a warp have, stored in words and element by element."""
+    _run(np.random.default_rng(n), n, 640, out, yt=yt, bt=F32, pady=pady)
+
+
+@pytest.mark.parametrize("n", [5, 41, 100, 127])
+@pytest.mark.parametrize("k", [512, 513])
+def test_few_rows_that_fill_part_of_a_warp(n, k):
+    """The same of the kernel that divides K, and of its form for rows that bulk copies cannot fetch."""
+    _run(np.random.default_rng(n), n, k, 1031, yt=F16, bt=F16)
