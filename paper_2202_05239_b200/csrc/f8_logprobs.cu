@@ -525,6 +525,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
             }
         }
     }
+    __syncwarp();                           // the barrier of the cluster takes all lanes together
     if (CLUSTER) cluster_sync();            // no block goes while the leader may read it
 }
 

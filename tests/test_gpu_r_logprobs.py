@@ -311,3 +311,13 @@ def test_networks_of_few_classes(classes, batch, top):
     tol, _ = _bounds(want, h, classes)
     assert bool(((lp.double() - want.gather(1, order)).abs() <= tol.gather(1, order)).all())
     net.close()
+
+
+@pytest.mark.parametrize("tokens,top", [(1, 1), (3, 5), (33, 31), (0, 7)])
+def test_lanes_of_the_leading_block_have_different_work(tokens, top):
+    """Rows shared by the blocks of a cluster, outputs that only some lanes of a warp write, rows ranked in one pass and by a pass for each
+    alternative side by side."""
+    logits = _logits(np.random.default_rng(top), 9, 80001, BF16)
+    for fill in (0.0, 1.5):
+        logits[::2] = fill              # equal logits: more candidates than there is room for
+        _run(logits, tokens=tokens, top=top)
