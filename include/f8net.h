@@ -351,6 +351,7 @@ f8_status f8_format_study_fixed(const float *x, long long n, int is_unsigned, do
  *         q = floor(v * i + 1/2) in [-127, 127]       (the product exact: round half up as everywhere in this library)
  *     and the value a code stands for is q * s.  A row with a < 2^-100 is a row of zeros: s = 0, q = 0.  A row that holds an
  *     infinity or a NaN has s = a / 127 (so infinite or NaN) and q = 0: each of its values, and each product made of it, is NaN.
+ *   - A row has at most 2^31 - 256 elements, a call at most 2^31 - 1 rows (F8_ERR_SHAPE).
  *   - An output may be the memory of an input of the same size of element and the same row distance (in place); other overlaps of
  *     outputs with inputs or with each other are not allowed.
  *   - Nothing is kept from call to call, no memory is allocated, and every call can be captured into a graph (f8_linear_scaled: after

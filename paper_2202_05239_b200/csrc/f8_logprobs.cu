@@ -563,7 +563,8 @@ extern "C" f8_status f8_token_logprobs(const f8_logprobs_desc *desc, const void 
                                        float *top_logprobs, int64_t *top_ids, void *cuda_stream) {
     if (!desc) return f8_set_error(F8_ERR_NULL, "descriptor is NULL");
     f8_logprobs_desc d = *desc;
-    if (d.n < 0 || d.n > 0x7fffffffll || d.v <= 0 || d.tokens < 0) return f8_set_error(F8_ERR_SHAPE, "n in 0 .. 2^31 - 1, v > 0 and tokens >= 0 are needed");
+    if (d.n < 0 || d.n > 0x7fffffffll || d.v <= 0 || d.v > MOST_EXTENT || d.tokens < 0 || d.tokens > MOST_EXTENT)
+        return f8_set_error(F8_ERR_SHAPE, "n in 0 .. 2^31 - 1, v in 1 .. 2^31 - 256 and tokens in 0 .. 2^31 - 256 are needed");
     if (d.top < 0 || d.top > 32 || d.top > d.v) return f8_set_error(F8_ERR_SHAPE, "top must be in 0 .. 32 and at most v");
     if (!(d.inv_temperature > 0.f) || !isfinite(d.inv_temperature)) return f8_set_error(F8_ERR_SHAPE, "inv_temperature must be positive and finite");
     const int size = d.dtype == F8_S32 ? 4 : real_size(d.dtype);

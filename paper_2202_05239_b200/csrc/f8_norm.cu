@@ -498,7 +498,7 @@ extern "C" f8_status f8_norm_quantize(const f8_norm_desc *desc, const void *x, c
                            void *y, void *cuda_stream) {
     if (!desc) return f8_set_error(F8_ERR_NULL, "descriptor is NULL");
     f8_norm_desc d = *desc;
-    if (d.n < 0 || d.n > 0x7fffffffll || d.c <= 0) return f8_set_error(F8_ERR_SHAPE, "n in 0 .. 2^31 - 1 and c > 0 are needed");
+    if (d.n < 0 || d.n > 0x7fffffffll || d.c <= 0 || d.c > MOST_EXTENT) return f8_set_error(F8_ERR_SHAPE, "n in 0 .. 2^31 - 1 and c in 1 .. 2^31 - 256 are needed");
     const int size = real_size(d.dtype);
     if (!size) return f8_set_error(F8_ERR_DTYPE, "dtype must be F8_F32, F8_F16 or F8_BF16");
     if (d.w_dtype != F8_F32 && d.w_dtype != d.dtype) return f8_set_error(F8_ERR_DTYPE, "w_dtype must be F8_F32 or dtype");

@@ -92,6 +92,9 @@ struct RowScale {
     __device__ __forceinline__ int code(float v) const { return __float2int_rd(__fmaf_rd(v, inverse, 0.5f)); }
 };
 
+// Longest extent of a row: the loops over rows of any length count in 32 bits, up to a block's step beyond the last element.
+constexpr int MOST_EXTENT = 0x7fffff00;
+
 inline int real_size(int dtype) { return dtype == F8_F32 ? 4 : (dtype == F8_F16 || dtype == F8_BF16 ? 2 : 0); }
 
 // Launch whose blocks may start while what is before them in the stream drains; the kernels wait before they touch memory.

@@ -133,3 +133,14 @@ def test_binding_refuses_wrong_tensors():
         api.f8_norm_quantize(torch.zeros(4, 64))
     with pytest.raises(ValueError):
         api.f8_token_logprobs(torch.zeros(4, 64, dtype=torch.int8))
+
+
+@pytest.mark.parametrize("extent,status", [(2 ** 31 - 255, 2), (2 ** 31 - 1, 2), (2 ** 31 - 256, 6)])
+def test_longest_rows(extent, status):
+    """Rows that the kernels could not count through in 32 bits are refused; the longest others come as far as the check of their pointers."""
+    b = ctypes.byref
+    assert api._lib.f8_quantize_rows(b(_rows(c=extent, n=1)), ODD, A, A, A, A, None) == status
+    assert api._lib.f8_norm_quantize(b(_norm(c=extent, n=1, gate_rows=1)), ODD, *([A] * 10), None) == status
+    assert api._lib.f8_token_logprobs(b(_lp(v=extent, n=1)), ODD, A, A, A, A, A, None) == status
+    assert api._lib.f8_token_logprobs(b(_lp(tokens=extent, n=1)), ODD, A, A, A, A, A, None) == status
+    assert api._lib.f8_linear_scaled(b(_scaled(out=extent, w_scales=1, n=1, x_scales=1)), A, ODD, A, A, A, A, None) == status
