@@ -130,10 +130,11 @@ struct Sums {
         s = add2(s, pair(e, 0.f));
         t = fma2(pair(e, 0.f), pair(fmaxf(d, -3e38f), 0.f), t);
     }
-    // the sums relative to a larger m (which is none of the elements met so far)
+    // the sums relative to a larger m (which is none of the elements met so far).  f d first, which is small wherever f is: s d of a mask of
+    // low numbers is -infinity, and 0 times that NaN.
     __device__ __forceinline__ void raise(V to, float cl) {
         const float d = fmaxf(Num<T>::minus(m, to), -3e38f), f = exp2_fast(d * cl);
-        t = mul2(both(f), fma2(s, both(d), t));
+        t = fma2(s, both(f * d), mul2(both(f), t));
         s = mul2(s, both(f));
         m = to;
     }
@@ -317,9 +318,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         if (some) {
             const float d = lost ? 0.f : fmaxf(N::minus(sum.m, m), -3e38f), f = exp2_fast(d * cl);
             const float own_s = sum.sum_s(), own_t = sum.sum_t();
-            t = f * fmaf(own_s, d, own_t);
+            t = fmaf(own_s, f * d, f * own_t);              // (see raise)
             s = owner ? 0.f : f * own_s;
-            if (f == 0.f && own_s == own_s) s = t = 0.f;
             if (owner && own_s != own_s) s = own_s;
         }
         keys[tid] = high;
@@ -469,8 +469,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
                     t += bt;
                 } else {
                     const float d = lost ? 0.f : fmaxf(N::minus(N::value((uint32_t)(k >> 32)), m), -3e38f), f = exp2_fast(d * cl);
-                    r += f == 0.f && br == br ? 0.f : f * (1.f + br);
-                    t += f == 0.f && br == br ? 0.f : f * fmaf(1.f + br, d, bt);
+                    r += f * (1.f + br);
+                    t += fmaf(1.f + br, f * d, f * bt);
                 }
             }
             best = top;

@@ -321,3 +321,25 @@ def test_lanes_of_the_leading_block_have_different_work(tokens, top):
     for fill in (0.0, 1.5):
         logits[::2] = fill              # equal logits: more candidates than there is room for
         _run(logits, tokens=tokens, top=top)
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("n,v", [(8, 1003), (8, 5001), (400, 20003), (8, 140001)])      # in registers, by a block, by many, by a cluster
+def test_masks_of_low_numbers_in_front(n, v, t):
+    """Threads that have met nothing but a mask of finite low numbers, then an open place: the mask adds nothing, and no NaN."""
+    rng = np.random.default_rng(v)
+    for low in (torch.finfo(t).min, -1e38, -6e4):
+        low = max(low, torch.finfo(t).min)
+        logits = _logits(rng, n, v, t)
+        logits[0, :-5] = low
+        logits[1, :-1] = low                                    # one open place, behind the last whole vector
+        logits[2, : v // 2] = low
+        logits[3, v // 3:] = low
+        stretch = 1024 * 16 // logits.element_size()
+        logits[4, torch.arange(v, device="cuda") // stretch % 2 == 0] = low
+        logits[5] = low                                         # equal logits, low as they are
+        logits[6] = low
+        logits[6, v // 2] = -1e4
+        logits[7:, ::3] = low
+        _run(logits, tokens=3, top=20)
+        assert bool((_run(logits, tokens=1, top=1) >= 0).all())
