@@ -419,6 +419,7 @@ f8_status f8_norm_quantize(const f8_norm_desc *desc, const void *x, const void *
  *   A token below 0 is a padded place: its log probability is 0.  One at or beyond v has NaN.  Logits of -infinity have probability 0; a
  *   row of nothing else has log probabilities of -infinity (its top_ids are 0, 1, ...) and entropy 0.  A row that holds
  *   a NaN or +infinity has NaN in every log probability and in its entropy; NaN sorts before +infinity.
+ *   Logits further below the largest than the largest 32-bit float, whatever the temperature, count as -infinity.
  * Errors: F8_ERR_NULL, F8_ERR_SHAPE (also an inv_temperature that is not positive and finite), F8_ERR_DTYPE, F8_ERR_FL_RANGE (fl outside
  * [-8, 32]), F8_ERR_ALIGN, F8_ERR_TIMEOUT. */
 typedef struct {

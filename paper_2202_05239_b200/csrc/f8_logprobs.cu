@@ -111,7 +111,8 @@ template <> struct Num<int> {
     static __device__ __forceinline__ bool empty(uint32_t) { return false; }
 };
 
-// Sums over some of the elements x relative to m: s of exp((x - m) c), t of (x - m) exp((x - m) c), each in two halves.
+// Sums over some of the elements x relative to m: with z = (x - m) c log2(e), s of 2^z and t of z 2^z, each in two halves.  (t in z and not in
+// x - m: of that the sum over a row passes the largest float where c is small and the logits are as large.)
 template <typename T>
 struct Sums {
     typedef typename Num<T>::V V;
@@ -119,22 +120,21 @@ struct Sums {
     F2 s, t;
     // two more elements, at most m
     __device__ __forceinline__ void add(V x, V y, V ref, float cl) {
-        const F2 d = Num<T>::minus2(x, y, ref);
-        const float2 z = halves(mul2(d, both(cl))), f = halves(d);
+        const float2 z = halves(mul2(Num<T>::minus2(x, y, ref), both(cl)));
         const F2 e = pair(exp2_fast(z.x), exp2_fast(z.y));
         s = add2(s, e);
-        t = fma2(e, pair(fmaxf(f.x, -3e38f), fmaxf(f.y, -3e38f)), t);       // (0 * infinity)
+        t = fma2(e, pair(fmaxf(z.x, -3e38f), fmaxf(z.y, -3e38f)), t);       // (0 * infinity)
     }
     __device__ __forceinline__ void add(V x, V ref, float cl) {
-        const float d = Num<T>::minus(x, ref), e = exp2_fast(d * cl);
+        const float z = Num<T>::minus(x, ref) * cl, e = exp2_fast(z);
         s = add2(s, pair(e, 0.f));
-        t = fma2(pair(e, 0.f), pair(fmaxf(d, -3e38f), 0.f), t);
+        t = fma2(pair(e, 0.f), pair(fmaxf(z, -3e38f), 0.f), t);
     }
-    // the sums relative to a larger m (which is none of the elements met so far).  f d first, which is small wherever f is: s d of a mask of
+    // the sums relative to a larger m (which is none of the elements met so far).  f z first, which is small wherever f is: s z of a mask of
     // low numbers is -infinity, and 0 times that NaN.
     __device__ __forceinline__ void raise(V to, float cl) {
-        const float d = fmaxf(Num<T>::minus(m, to), -3e38f), f = exp2_fast(d * cl);
-        t = fma2(s, both(f * d), mul2(both(f), t));
+        const float z = fmaxf(Num<T>::minus(m, to) * cl, -3e38f), f = exp2_fast(z);
+        t = fma2(s, both(f * z), mul2(both(f), t));
         s = mul2(s, both(f));
         m = to;
     }
@@ -316,9 +316,9 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
     {
         float s = 0.f, t = 0.f;
         if (some) {
-            const float d = lost ? 0.f : fmaxf(N::minus(sum.m, m), -3e38f), f = exp2_fast(d * cl);
+            const float z = lost ? 0.f : fmaxf(N::minus(sum.m, m) * cl, -3e38f), f = exp2_fast(z);
             const float own_s = sum.sum_s(), own_t = sum.sum_t();
-            t = fmaf(own_s, f * d, f * own_t);              // (see raise)
+            t = fmaf(own_s, f * z, f * own_t);              // (see raise)
             s = owner ? 0.f : f * own_s;
             if (owner && own_s != own_s) s = own_s;
         }
@@ -468,9 +468,9 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
                     r += br;
                     t += bt;
                 } else {
-                    const float d = lost ? 0.f : fmaxf(N::minus(N::value((uint32_t)(k >> 32)), m), -3e38f), f = exp2_fast(d * cl);
+                    const float z = lost ? 0.f : fmaxf(N::minus(N::value((uint32_t)(k >> 32)), m) * cl, -3e38f), f = exp2_fast(z);
                     r += f * (1.f + br);
-                    t += fmaf(1.f + br, f * d, f * bt);
+                    t += fmaf(1.f + br, f * z, f * bt);
                 }
             }
             best = top;
@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         const bool bad = r != r || t != t || !best || N::bad(top), empty = N::empty(top);
         const float nan = __int_as_float(0x7fffffff), lse = log1pf(r);
         auto logprob = [&](V x) { return bad ? nan : empty ? -INFINITY : N::minus(x, m) * p.c - lse; };
-        if (tid == 0 && p.entropy) p.entropy[row] = bad ? nan : empty ? 0.f : lse - t * p.c / (1.f + r);
+        if (tid == 0 && p.entropy) p.entropy[row] = bad ? nan : empty ? 0.f : lse - t * 0.693147181f / (1.f + r);        // ln 2
         if (p.lp)
             for (int j = tid; j < p.tokens; j += LP_THREADS) {
                 const int64_t id = p.ids[row * p.tokens + j];

@@ -343,3 +343,14 @@ def test_masks_of_low_numbers_in_front(n, v, t):
         logits[7:, ::3] = low
         _run(logits, tokens=3, top=20)
         assert bool((_run(logits, tokens=1, top=1) >= 0).all())
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,v", [(3, 1003), (3, 5001), (400, 20003), (3, 140001)])
+def test_large_logits_at_a_high_temperature(n, v, t):
+    """Logits near the largest float, which the temperature takes back: only their product with its inverse counts."""
+    rng = np.random.default_rng(v)
+    logits = (_logits(rng, n, v, F32) * 2.0 ** 122).to(t)
+    _run(logits, tokens=3, top=5, inv_t=2.0 ** -122)
+    logits[:, : v // 2] = torch.finfo(t).min / 4
+    _run(logits, tokens=3, top=5, inv_t=2.0 ** -122)
