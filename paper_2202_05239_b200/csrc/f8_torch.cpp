@@ -70,10 +70,12 @@ struct Matrix {
     void *p = nullptr;
     long long rows = 0, cols = 0, ld = 0;
     int dtype = 0;
+    bool given = false;         // (a tensor without elements may have no memory)
     Matrix() {}
     Matrix(Call &c, PyObject *o, const char *what, unsigned types, bool optional = false) {
         const at::Tensor *t = c.tensor(o, what, optional);
         if (!t) return;
+        given = true;
         dtype = dtype_of(*t, types, what);
         if (t->dim() != 2) refuse(what, "a matrix is needed");
         rows = t->size(0);
@@ -85,10 +87,10 @@ struct Matrix {
         p = const_cast<void *>(t->const_data_ptr());
     }
     void shaped(long long r, long long c, const char *what) const {
-        if (p && (rows != r || cols != c)) refuse(what, "its shape does not fit the other tensors'");
+        if (given && (rows != r || cols != c)) refuse(what, "its shape does not fit the other tensors'");
     }
     void typed(int d, const char *what) const {
-        if (p && dtype != d) refuse(what, "its type is not the other tensors'");
+        if (given && dtype != d) refuse(what, "its type is not the other tensors'");
     }
 };
 

@@ -133,3 +133,19 @@ def test_block_of_a_transformer(n, c, hidden, vocab):
     assert bool(((h.double() + (want.exp() * want).sum(dim=1)).abs() <= 1e-5 * (1 + h.double())).all())
     torch.cuda.synchronize()
     a.f8_device_status()
+
+
+def test_tensors_without_rows_do_not_count_as_left_out():
+    """An optional matrix that has no rows fits a call of no rows alone."""
+    a = api()
+    x, q, s = torch.randn(4, 64, device="cuda").to(BF16), torch.zeros(4, 64, dtype=S8, device="cuda"), torch.zeros(4, device="cuda")
+    none, no_codes = x[:0], q[:0]
+    for kw in (dict(u=none), dict(y=none), dict(q=no_codes, scale=None, y=x.clone())):
+        with pytest.raises(ValueError, match="shape"):
+            a.f8_quantize_rows(**{**dict(x=x, q=q, scale=s), **kw})
+    for kw in (dict(residual=none), dict(residual_out=none), dict(gate=none), dict(y=none), dict(q=no_codes, scale=None, y=x.clone())):
+        with pytest.raises(ValueError, match="shape"):
+            a.f8_norm_quantize(**{**dict(x=x, q=q, scale=s), **kw})
+    a.f8_quantize_rows(none, no_codes, s[:0], y=none, u=none)
+    a.f8_norm_quantize(none, no_codes, s[:0], y=none, residual=none, residual_out=none, gate=none)
+    a.f8_norm_quantize(none, no_codes, s[:0], gate=x[:1])
