@@ -126,6 +126,12 @@ float real(PyObject *o) {
     return (float)v;
 }
 
+// Lets other Python threads run, as a call through ctypes does: a launch waits where the queue of launches is full.
+struct OthersRun {
+    PyThreadState *state = PyEval_SaveThread();
+    ~OthersRun() { PyEval_RestoreThread(state); }
+};
+
 template <typename F>
 PyObject *guarded(Py_ssize_t got, Py_ssize_t want, F f) {
     if (got != want) {
@@ -150,7 +156,9 @@ PyObject *linear_scaled(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         y.shaped(x.rows, w.rows, "y");
         const Vector xs(c, a[1], "x_scale", F32, x.rows, true, false), ws(c, a[3], "w_scale", F32, w.rows, true, false), b(c, a[5], "bias", REAL, w.rows);
         f8_scaled_desc d = {(int)x.rows, (int)x.cols, (int)w.rows, x.dtype, y.dtype, b.p ? b.dtype : F8_F32, (int)xs.n, (int)ws.n, x.ld, w.ld, y.ld};
-        return f8_linear_scaled(&d, x.p, (const float *)xs.p, (const int8_t *)w.p, (const float *)ws.p, b.p, y.p, c.stream(a[6]));
+        const cudaStream_t stream = c.stream(a[6]);
+        const OthersRun others;
+        return f8_linear_scaled(&d, x.p, (const float *)xs.p, (const int8_t *)w.p, (const float *)ws.p, b.p, y.p, stream);
     });
 }
 
@@ -166,7 +174,9 @@ PyObject *quantize_rows(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         u.typed(x.dtype, "u");
         const Vector s(c, a[2], "scale", F32, x.rows);
         f8_rows_desc d = {x.rows, (int)x.cols, x.dtype, small(a[5]), x.ld, u.ld, y.ld, q.ld};
-        return f8_quantize_rows(&d, x.p, u.p, (int8_t *)q.p, (float *)s.p, y.p, c.stream(a[6]));
+        const cudaStream_t stream = c.stream(a[6]);
+        const OthersRun others;
+        return f8_quantize_rows(&d, x.p, u.p, (int8_t *)q.p, (float *)s.p, y.p, stream);
     });
 }
 
@@ -195,7 +205,9 @@ PyObject *norm_quantize(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         }
         f8_norm_desc d = {x.rows, (int)x.cols, x.dtype, wt >= 0 ? wt : F8_F32, small(a[8]), small(a[11]), small(a[7]), g.p ? g.rows : 1,
                           real(a[14]), real(a[15]), real(a[16]), x.ld, g.ld, r.ld, sum.ld, y.ld, q.ld};
-        return f8_norm_quantize(&d, x.p, g.p, r.p, post_w.p, post_b.p, pre_w.p, pre_b.p, sum.p, (int8_t *)q.p, (float *)s.p, y.p, c.stream(a[17]));
+        const cudaStream_t stream = c.stream(a[17]);
+        const OthersRun others;
+        return f8_norm_quantize(&d, x.p, g.p, r.p, post_w.p, post_b.p, pre_w.p, pre_b.p, sum.p, (int8_t *)q.p, (float *)s.p, y.p, stream);
     });
 }
 
@@ -216,7 +228,9 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
         const Vector ids(c, a[1], "tokens", I64, l.rows * tokens), lp(c, a[2], "logprobs", F32, l.rows * tokens), h(c, a[3], "entropy", F32, l.rows);
         const Vector tl(c, a[4], "top_logprobs", F32, l.rows * top), ti(c, a[5], "top_ids", I64, l.rows * top);
         f8_logprobs_desc d = {l.rows, (int)l.cols, l.dtype, small(a[6]), (int)tokens, (int)top, real(a[7]), l.ld};
-        return f8_token_logprobs(&d, l.p, (const int64_t *)ids.p, (float *)lp.p, (float *)h.p, (float *)tl.p, (int64_t *)ti.p, c.stream(a[8]));
+        const cudaStream_t stream = c.stream(a[8]);
+        const OthersRun others;
+        return f8_token_logprobs(&d, l.p, (const int64_t *)ids.p, (float *)lp.p, (float *)h.p, (float *)tl.p, (int64_t *)ti.p, stream);
     });
 }
 

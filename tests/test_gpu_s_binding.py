@@ -1,4 +1,7 @@
 """What the binding of the calls on real-valued tensors refuses, and a run of the calls together as a transformer's block makes them."""
+import threading
+import time
+
 import pytest
 import torch
 
@@ -149,3 +152,32 @@ def test_tensors_without_rows_do_not_count_as_left_out():
     a.f8_quantize_rows(none, no_codes, s[:0], y=none, u=none)
     a.f8_norm_quantize(none, no_codes, s[:0], y=none, residual=none, residual_out=none, gate=none)
     a.f8_norm_quantize(none, no_codes, s[:0], gate=x[:1])
+
+
+def test_other_threads_run_while_a_launch_waits_for_the_queue():
+    """A call that has to wait for room among the launches on their way does not stop the other Python threads."""
+    a = api()
+    x, q, s = torch.randn(1, 64, device="cuda"), torch.zeros(1, 64, dtype=S8, device="cuda"), torch.zeros(1, device="cuda")
+    a.f8_quantize_rows(x, q, s)
+    torch.cuda.synchronize()
+    ticks, done = [], threading.Event()
+
+    def tick():
+        while not done.is_set():
+            ticks.append(time.perf_counter())
+            time.sleep(0.002)
+    other = threading.Thread(target=tick)
+    other.start()
+    try:
+        torch.cuda._sleep(1_500_000_000)        # three quarters of a second or more of the GPU
+        start = time.perf_counter()
+        for _ in range(5000):                   # far more launches than the queue holds
+            a.f8_quantize_rows(x, q, s)
+        took = time.perf_counter() - start
+    finally:
+        done.set()
+        other.join()
+        torch.cuda.synchronize()
+    assert took > 0.4, "the queue was never full"
+    gap = max(b - a for a, b in zip(ticks, ticks[1:]))
+    assert gap < took / 4, f"another thread stood still for {gap:.2f} of {took:.2f} s"
