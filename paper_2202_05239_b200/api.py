@@ -4,7 +4,8 @@ Only argument marshalling happens here: every function forwards device pointers
 of torch tensors (torch supplies memory and streams) to the entry point of the
 same name in ``include/f8net.h`` (those on real-valued tensors through a C++
 module of this package, ``csrc/f8_torch.cpp``).  There is no CPU fallback: importing this
-module fails if the library has not been built.
+module fails if the library has not been built; without the C++ module, which is
+bound to one torch and one Python, the calls on real-valued tensors alone fail.
 """
 from __future__ import annotations
 
@@ -20,14 +21,29 @@ from . import synth
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libf8net.so")
 
-if not os.path.exists(_LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_f8torch.so")):
+if not os.path.exists(_LIB_PATH):
     raise ImportError(
-        f"{_LIB_PATH} or _f8torch.so is missing: build the CUDA library first "
+        f"{_LIB_PATH} is missing: build the CUDA library first "
         "(python -m paper_2202_05239_b200.build, or __graft_entry__.build())")
 
 _lib = ctypes.CDLL(_LIB_PATH)
 
-from . import _f8torch  # noqa: E402  (built beside the library; needs it and torch loaded)
+
+class _Unavailable:
+    """In the place of the C++ module where it cannot be loaded: every use says why."""
+
+    def __init__(self, error):
+        self._error = error
+
+    def __getattr__(self, name):
+        raise ImportError("the calls on real-valued tensors need _f8torch.so built for this torch and this Python "
+                          f"(python -m {__package__}.build): {self._error}")
+
+
+try:
+    from . import _f8torch  # noqa: E402  (built beside the library; needs it and torch loaded)
+except ImportError as _e:
+    _f8torch = _Unavailable(_e)
 
 F8_OK = 0
 F8_U8, F8_S8, F8_S32, F8_S32_RELU = 0, 1, 2, 3
