@@ -4,6 +4,7 @@ from __future__ import annotations
 import glob
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -21,19 +22,32 @@ def _newest_source_mtime() -> float:
     return max(os.path.getmtime(f) for f in files)
 
 
+def binding_made_for() -> str:
+    """The Python and the torch that the binding is bound to: the module holds this text."""
+    import torch
+    return "made for %s, torch %s;" % (sysconfig.get_config_var("SOABI"), torch.__version__)
+
+
+def binding_is_current() -> bool:
+    """Whether the module is there, newer than what it is made of and made for this Python and this torch."""
+    made_of = [os.path.join(CSRC, "f8_torch.cpp"), os.path.join(os.path.dirname(HERE), "include", "f8net.h")]
+    if not os.path.exists(BINDING) or os.path.getmtime(BINDING) < max(os.path.getmtime(f) for f in made_of):
+        return False
+    with open(BINDING, "rb") as f:
+        return binding_made_for().encode() in f.read()
+
+
 def build_binding(force: bool = False) -> str:
     """The calls on torch tensors that are made from C++ (csrc/f8_torch.cpp), linked against torch and the library."""
-    source = os.path.join(CSRC, "f8_torch.cpp")
-    header = os.path.join(os.path.dirname(HERE), "include", "f8net.h")
-    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(os.path.getmtime(source), os.path.getmtime(header)):
+    if not force and binding_is_current():
         return BINDING
-    import sysconfig
-
     import torch
+    source = os.path.join(CSRC, "f8_torch.cpp")
     at = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     tmp = BINDING + ".tmp%d" % os.getpid()
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-o", tmp, source,
+                           '-DF8_MADE_FOR="%s"' % binding_made_for(),
                            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
                            "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
                            "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(cuda, "include"),

@@ -239,7 +239,8 @@ PyMethodDef methods[] = {{"linear_scaled", (PyCFunction)(void (*)())linear_scale
                          {"norm_quantize", (PyCFunction)(void (*)())norm_quantize, METH_FASTCALL, nullptr},
                          {"token_logprobs", (PyCFunction)(void (*)())token_logprobs, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_f8torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+// (the text by which the build knows whether the module was made for the Python and the torch at hand)
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_f8torch", "Calls on torch tensors, " F8_MADE_FOR, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }   // namespace
 

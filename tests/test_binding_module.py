@@ -34,3 +34,21 @@ def test_fixed_point_path_without_the_module(tmp_path, module):
         "        raise AssertionError(call)\n")
     run = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env={**os.environ, "PYTHONPATH": str(tmp_path)}, capture_output=True, text=True)
     assert run.returncode == 0, run.stderr
+
+
+def test_module_is_built_again_for_another_torch_or_python(monkeypatch):
+    """A module made for another torch or another Python does not load, however new its file is."""
+    from paper_2202_05239_b200 import api, build
+    assert build.binding_is_current()
+    assert build.binding_made_for() in api._f8torch.__doc__
+    import torch
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", torch.__version__ + "1")
+        assert not build.binding_is_current()
+    with monkeypatch.context() as m:
+        m.setattr(build.sysconfig, "get_config_var", lambda name: "cpython-399-none")
+        assert not build.binding_is_current()
+    with monkeypatch.context() as m:
+        m.setattr(build, "BINDING", build.BINDING + ".none")
+        assert not build.binding_is_current()
+    assert build.binding_is_current()
