@@ -62,8 +62,6 @@ __device__ __forceinline__ int key_index(Key k) { return (int)~(uint32_t)k; }
 
 struct MaxOp { __device__ __forceinline__ Key operator()(Key a, Key b) const { return a > b ? a : b; } };
 
-__device__ __forceinline__ float exp2_fast(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
-
 // What differs between real logits and codes: the largest value is a float or an integer, and so is the difference before it is rounded.
 template <typename T> struct Num {
     typedef float V;

@@ -11,6 +11,7 @@ from scaled_util import U, check_codes, gelu, half_step, norm64, same_codes, sil
 pytestmark = pytest.mark.gpu
 
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+INF = float("inf")
 SHAPES = [(1, 1), (1, 2), (3, 7), (5, 16), (2, 63), (4, 64), (9, 100), (17, 256), (3, 513), (6, 1024), (2, 1537), (7, 2048), (3, 4100), (2, 8192), (1, 16384), (2, 16385),
           (1, 40001)]
 
@@ -352,3 +353,56 @@ def test_no_rows():
     x = torch.zeros(0, 64, device="cuda")
     a.f8_quantize_rows(x, torch.zeros(0, 64, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda"))
     a.f8_norm_quantize(x, torch.zeros(0, 64, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda"))
+
+
+def _every_number(t):
+    return torch.arange(-2 ** 15, 2 ** 15, dtype=torch.int32).to(torch.int16).view(t).cuda()
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+def test_silu_of_every_number_is_a_32_bit_result(t):
+    """The scale of a row is a 32-bit number: of rows of one element each it shows the activation's own error."""
+    a = api()
+    x = _every_number(t)
+    x = x[torch.isfinite(x) & (x > -88.7)].view(-1, 1).contiguous()         # (below, exp(-x) is infinite in 32 bits)
+    # a gate that brings the far ends back into range: a power of two, exact
+    u = torch.where(x < -40, 2.0 ** 60 if t == BF16 else 2.0 ** 15, torch.where((x.abs() < 2.0 ** -60), 2.0 ** 60, 1.0)).to(t)
+    q, s = torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(x.shape[0], device="cuda")
+    a.f8_quantize_rows(x, q, s, u=u, act=a.F8_ACT_SILU)
+    want = (silu(x.double()) * u.double())[:, 0].abs()
+    some = want >= 2.0 ** -100 * (1 + 2.0 ** -16)
+    # exponential and reciprocal within 2^-22 and 2^-23, four roundings between them, the gate and the division of the scale: 4 + 2 + 6 half steps
+    assert bool(((s.double() - want / 127).abs() <= 1.01 * 12 * U * want / 127)[some].all())
+    assert int(some.sum()) > (30000 if t == BF16 else 40000) and bool((s[want < 2.0 ** -100 * (1 - 2.0 ** -16)] == 0).all())
+
+
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+def test_silu_far_out_and_not_finite(t):
+    a = api()
+    far = torch.finfo(t).max
+    x = torch.tensor([[far, -far, INF, -INF, float("nan"), 200.0, -200.0, 126.0, -126.0, 0.0, -0.0, -87.5, -88.5]], device="cuda").to(t)
+    for c in (1, 20000):                            # in registers, and a row of any length
+        rows = x.t().expand(-1, c).contiguous()
+        y = torch.empty_like(rows)
+        a.f8_quantize_rows(rows, y=y, act=a.F8_ACT_SILU)
+        y = y.double()
+        assert bool((y == y[:, :1]).logical_or(y.isnan()).all())
+        got = y[:, 0].tolist()
+        assert got[0] == far and got[1] == 0 and got[2] == INF and got[3] != got[3] and got[4] != got[4]
+        assert got[5] == 200 and got[6] == 0 and got[7] == 126 and abs(got[8]) < 1e-36 and got[9] == 0 and got[10] == 0
+        for i in (11, 12):
+            z = silu(x[0, i].double()).item()
+            assert abs(got[i] - z) <= (half_step(t) + 12 * U) * abs(z) + tiny(t) + 1e-45
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("c", [100, 3000, 20000])
+def test_scales_of_negative_activations(t, c):
+    """Rows whose values are all far below zero, where the exponential of a rounded product would be off by the size of the product."""
+    a = api()
+    rng = np.random.default_rng(c)
+    x = torch.from_numpy(rng.uniform(-35, -15, size=(20, c)) if t == BF16 else rng.uniform(-16, -8, size=(20, c))).to(t).cuda()
+    q, s = torch.empty(20, c, dtype=torch.int8, device="cuda"), torch.empty(20, device="cuda")
+    a.f8_quantize_rows(x, q, s, act=a.F8_ACT_SILU)
+    v = silu(x.double())
+    check_codes(v, v.abs() * 11 * U, q, s)
