@@ -50,7 +50,7 @@ __device__ __forceinline__ V block_reduce(V v, Op op, V *room) {
     constexpr int WARPS = THREADS / 32;
     if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
     __syncthreads();
-    if (WARPS <= 8) {
+    if (WARPS <= 8 || (WARPS & (WARPS - 1)) != 0) {
         v = room[0];
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) v = op(v, room[w]);

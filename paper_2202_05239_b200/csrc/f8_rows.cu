@@ -51,7 +51,8 @@ __global__ void __launch_bounds__(ROW_THREADS) long_quantize_kernel(RowsParams p
 // special function units, each within 2^-22.  -v log2(e) is rounded to t, which alone would put the exponential off by |v| 2^-24; what the
 // rounding left out comes from a multiply-add, exactly, and goes in to first order: exp(-v) = 2^t (1 - left ln 2).  The quarter keeps the
 // reciprocal above the smallest normal number wherever exp(-v) is finite, as in the plain form (v > -88.7); an infinite one gives 0.
-// 4096 x 8192 bf16, gated, codes and values: 38.2 us, with expf and a division 50.2; codes alone 32.8 and 44.9.
+// 4096 x 8192 bf16, gated, codes and values, the same buffers again and again: 38.2 us, with expf and a division 50.2, with the fast exponential and
+// quotient 38.7 (42.7 and 42.2 on new buffers each time); codes alone 32.8, 44.9 and 33.5.
 template <typename T>
 __device__ __forceinline__ F2 activate_two(F2 v, int act) {
     const float2 f = halves(v);
@@ -149,12 +150,21 @@ cudaError_t launch_row_quantize_at(const RowsParams &p, long long n, cudaStream_
 template <typename T, bool ACT, RowMode MODE>
 cudaError_t launch_row_quantize(const RowsParams &p, long long n, cudaStream_t st) {
     const int need = p.c + (MODE == SHIFT ? 16 / (int)sizeof(T) - 1 : 0);
+    // As few threads as hold the row, in steps of a quarter and a half between powers of two: threads beyond a row's end cost as much as
+    // the others.  Codes alone of 16 M elements, so and with powers of two only (us): rows of 1030 float 17.0 / 22.8, 1536 bf16 7.3 / 9.0, 2047
+    // float 14.9 / 23.7, 2304 bf16 8.5 / 11.5, 5000 bf16 9.0 / 11.8, 6000 float 10.7 / 12.8, 8191 bf16 13.8 / 20.5, 11008 bf16 9.7 / 11.6.
     if (need <= 32 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 32>(p, n, st);
     if (need <= 64 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 64>(p, n, st);
+    if (need <= 96 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 96>(p, n, st);
     if (need <= 128 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 128>(p, n, st);
-    if (need <= 160 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 160>(p, n, st);      // (just over 2048: a row of odd width, shifted)
+    if (need <= 160 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 160>(p, n, st);
+    if (need <= 192 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 192>(p, n, st);
     if (need <= 256 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 256>(p, n, st);
+    if (need <= 320 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 320>(p, n, st);
+    if (need <= 384 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 384>(p, n, st);
     if (need <= 512 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 512>(p, n, st);
+    if (need <= 640 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 640>(p, n, st);
+    if (need <= 768 * ROW_E) return launch_row_quantize_at<T, ACT, MODE, 768>(p, n, st);
     return launch_row_quantize_at<T, ACT, MODE, 1024>(p, n, st);
 }
 

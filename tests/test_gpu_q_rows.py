@@ -406,3 +406,25 @@ def test_scales_of_negative_activations(t, c):
     a.f8_quantize_rows(x, q, s, act=a.F8_ACT_SILU)
     v = silu(x.double())
     check_codes(v, v.abs() * 11 * U, q, s)
+
+
+@pytest.mark.parametrize("t", [BF16, F32])
+@pytest.mark.parametrize("c", [480, 1000, 1500, 2040, 2500, 3000, 4000, 5000, 6100, 8000, 10000, 12200, 16000])
+def test_every_number_of_threads(c, t):
+    """Rows that take every number of threads a block may have, some elements short of all of them, in each of the layouts; with rows in every block's
+    second round."""
+    a = api()
+    rng = np.random.default_rng(c)
+    n = 1200
+    for width, pad, offset in ((c, 0, 0), (c - 1, 0, 1), (c - 3, 2, 0)):
+        x, _ = strided(n, width, t, pad, offset)
+        x.copy_(_values(rng, n, width, t))
+        x[::7] *= 100
+        x[5, width - 1] = 1000          # the largest of its row is the last element, of another the first
+        x[6, 0] = -1000
+        q, s, y = torch.empty(n, width, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, width, dtype=t, device="cuda")
+        a.f8_quantize_rows(x, q, s, y=y)
+        same_codes(x.float(), q, s, y)
+        u = _values(rng, n, width, t)
+        a.f8_quantize_rows(x, q, s, u=u)
+        same_codes(x.float() * u.float(), q, s)
