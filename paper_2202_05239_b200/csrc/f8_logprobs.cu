@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
     constexpr int VEC = N::VEC;
     __shared__ Key room[2][32];
     __shared__ float froom[2][32];
-    __shared__ Key keys[LP_THREADS], found[LP_CANDIDATES];
+    __shared__ Key keys[LP_MOST_TOP], found[LP_CANDIDATES];          // the row's alternatives; what they are taken from
     __shared__ int members[LP_THREADS];
     __shared__ int counts[4];               // candidates; threads to read again; the owner of the largest element; threads worth a look
     __shared__ LpPart part;
@@ -320,7 +320,6 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
             s = owner ? 0.f : f * own_s;
             if (owner && own_s != own_s) s = own_s;
         }
-        keys[tid] = high;
         __syncthreads();
         // the owner's elements once more, by all threads: exp of all but the first that equals the largest
         const int who = counts[2];

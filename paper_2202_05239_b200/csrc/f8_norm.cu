@@ -10,6 +10,8 @@
 // 4096 x 8192 bf16, norms on both sides, channel gate, all outputs: 55 us, 5.5 TB/s.  On the way there: 32 elements a thread and the weights
 // read again for every row 73 us (half of them came from the second-level cache); 16 elements, several rows a block and the
 // factors in shared memory 72; 8 elements, one row at a time 64; two rows with the options of the call tested for each 58.
+// The deviation comes from rsqrtf (within 2^-22) and the mean from a product with 1 / c (two roundings): each thread of a row works both out, and
+// with sqrtf and divisions, half a step closer, the same call takes 58.9 us against 54.7.
 // Longer rows take a kernel that reads the row again for every sum, from the caches.
 #include "f8_rowdeal.cuh"
 
@@ -136,7 +138,7 @@ __device__ __forceinline__ void row_sums(float (&v)[R], float (*room)[32]) {
         v[1] = __shfl_sync(0xffffffffu, w, 16);
     }
 }
-// The same with the largest of a magnitude each beside the sums (sum: whether there are sums).
+// The largest of a magnitude each, in two halves with a barrier between them (that of the sums, where there are any): `wait` is the second.
 template <int THREADS, int R>
 __device__ __forceinline__ void row_peaks(uint32_t (&top)[R], uint32_t (*room)[32], bool wait) {
     constexpr int WARPS = THREADS / 32;
