@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from gpu_util import api
+from paper_2202_05239_b200 import synth
 from scaled_util import check_codes, norm64, silu
 
 pytestmark = pytest.mark.gpu
@@ -181,3 +182,58 @@ def test_other_threads_run_while_a_launch_waits_for_the_queue():
     assert took > 0.4, "the queue was never full"
     gap = max(b - a for a, b in zip(ticks, ticks[1:]))
     assert gap < took / 4, f"another thread stood still for {gap:.2f} of {took:.2f} s"
+
+
+def test_calls_on_several_streams_at_once():
+    """Products by every kernel, rows, log probabilities and a network's forward passes on streams of their own give what they give alone."""
+    a = api()
+    g = torch.Generator(device="cuda").manual_seed(0)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda")       # noqa: E731
+    codes = lambda *s: torch.randint(-127, 128, s, generator=g, device="cuda", dtype=S8)       # noqa: E731
+    one = torch.full((1,), 0.01, device="cuda")
+
+    def product(n, k, out):
+        x, w = codes(n, k), codes(out, k)
+
+        def call():
+            y = torch.empty(n, out, dtype=BF16, device="cuda")
+            a.f8_linear_scaled(x, one, w, one, y)
+            return [y]
+        return call
+
+    def rows(n, c):
+        x, r, u, w = rand(n, c).to(BF16), rand(n, c).to(BF16), rand(n, c).to(BF16), rand(c)
+
+        def call():
+            q, s, t, p, z = torch.empty(n, c, dtype=S8, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty(n, c, dtype=S8, device="cuda"), torch.empty(n, device="cuda")
+            a.f8_norm_quantize(x, q, s, residual=r, residual_out=t, pre_w=w)
+            a.f8_quantize_rows(t, p, z, u=u, act=a.F8_ACT_SILU)
+            return [q, s, t, p, z]
+        return call
+
+    def logprobs(n, v):
+        logits = rand(n, v)
+
+        def call():
+            h, ti = torch.empty(n, device="cuda"), torch.empty(n, 20, dtype=torch.int64, device="cuda")
+            a.f8_token_logprobs(logits, entropy=h, top_ids=ti)
+            return [h, ti]
+        return call
+    layers = synth.make_net("resnet50", 0, image=96)
+    net, images = a.Net(layers, 16), a.to_device(synth.draw_image(16, 1, 96, 96))
+    chains = [[product(1, 4096, 4096), product(23, 4096, 2048), product(100, 2048, 1000)], [product(2048, 1024, 2048), product(40, 1025, 999)],
+              [rows(700, 2048), logprobs(16, 131072), logprobs(3000, 1000)], [lambda: [net.forward(images)]]]
+    alone = [[call() for call in chain] for chain in chains]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in chains]
+    results = []
+    for _ in range(20):
+        for i, (stream, chain) in enumerate(zip(streams, chains)):
+            with torch.cuda.stream(stream):
+                results.append((i, [call() for call in chain]))
+    torch.cuda.synchronize()
+    a.f8_device_status()
+    for i, got in results:
+        for x, y in zip(alone[i], got):
+            assert all(torch.equal(p, q) for p, q in zip(x, y)), f"stream {i}"
+    net.close()
