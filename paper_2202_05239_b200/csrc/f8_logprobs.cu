@@ -40,7 +40,7 @@ constexpr int LP_MOST_TOP = 32;
 
 struct LpParams {
     int v, tokens, top;
-    float c;
+    float c, cl, back;                      // inverse temperature, the same times log2(e), and c / cl (of cl as it is, rounded)
     long long ldl;
     const void *logits;
     const int64_t *ids;
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
     const long long row = CLUSTER ? blockIdx.y : blockIdx.x;
     const uint32_t rank = CLUSTER ? cluster_rank() : 0u, ranks = CLUSTER ? gridDim.x : 1u;
     const T *l = (const T *)p.logits + row * p.ldl;
-    const float cl = p.c * 1.44269504f;
+    const float cl = p.cl;
     // the row: `head` elements in front of the first multiple of 16 bytes, whole vectors, `tail` elements; this block's part of them
     const int off = (int)((uintptr_t)l / sizeof(T) % VEC);
     const int head_all = off ? min(VEC - off, p.v) : 0, vecs_all = (p.v - head_all) / VEC;
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_BLOCKS) logprobs_kernel(LpParam
         const bool bad = r != r || t != t || !best || N::bad(top), empty = N::empty(top);
         const float nan = __int_as_float(0x7fffffff), lse = log1pf(r);
         auto logprob = [&](V x) { return bad ? nan : empty ? -INFINITY : N::minus(x, m) * p.c - lse; };
-        if (tid == 0 && p.entropy) p.entropy[row] = bad ? nan : empty ? 0.f : lse - t * 0.693147181f / (1.f + r);        // ln 2
+        if (tid == 0 && p.entropy) p.entropy[row] = bad ? nan : empty ? 0.f : lse - t * p.back / (1.f + r);
         if (p.lp)
             for (int j = tid; j < p.tokens; j += LP_THREADS) {
                 const int64_t id = p.ids[row * p.tokens + j];
@@ -579,7 +579,8 @@ extern "C" f8_status f8_token_logprobs(const f8_logprobs_desc *desc, const void 
         (((uintptr_t)logprobs | (uintptr_t)entropy | (uintptr_t)top_logprobs) & 3))
         return f8_set_error(F8_ERR_ALIGN, "a pointer is not aligned to its element");
     if (f8_pending_timeout() != F8_OK) return F8_ERR_TIMEOUT;
-    LpParams p = {d.v, d.tokens, top_logprobs || top_ids ? d.top : 0, c, d.ldl, logits, tokens, logprobs, entropy, top_logprobs, top_ids};
+    const float cl = c * 1.44269504f;
+    LpParams p = {d.v, d.tokens, top_logprobs || top_ids ? d.top : 0, c, cl, (float)((double)c / cl), d.ldl, logits, tokens, logprobs, entropy, top_logprobs, top_ids};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = d.dtype == F8_S32   ? launch_logprobs<int>(p, d.n, st)
                           : d.dtype == F8_F32 ? launch_logprobs<float>(p, d.n, st)
