@@ -13,6 +13,9 @@
 // The deviation comes from rsqrtf (within 2^-22) and the mean from a product with 1 / c (two roundings): each thread of a row works both out, and
 // with sqrtf and divisions, half a step closer, the same call takes 58.9 us against 54.7.
 // Longer rows take a kernel that reads the row again for every sum, from the caches.
+// One row at a time: codes alone of 4096 x 8192 bf16 (RMS norm 40.2 us with two rows) take 49.4 us with a gate per token, 66.2 with a layer norm and its
+// bias, and 149 where the rows are 8191 wide.  Above 8192 elements the weights are read again for every row (2048 x 16384 bf16: 78.2 us); 32-bit rows of that
+// length with a residual find no room for the next row in shared memory (2048 x 16384 float: 118 us); rows of any length, 2048 x 20000 bf16: 434 us.
 #include "f8_rowdeal.cuh"
 
 namespace {

@@ -6,6 +6,10 @@
 // Bound by memory traffic: every element is read and written once.  Rows of up to 16384 elements stay in registers, 16 elements a
 // thread, a warp to 32 warps a row, while the next row is on its way; longer ones take a kernel that reads the row
 // twice, the second time from the caches.
+// 4096 x 8192 bf16, gate and value with silu, codes alone: 32.6 us, 5.1 TB/s; with the values too 38.1. The forms that few calls take are far from
+// that: tensors whose rows lie differently against 16 bytes (halves of a tensor 2 x 8190 wide), element by element, 88.7 and 102 us; 32-bit rows of more
+// than 12288 elements with a gate, whose next row finds no room in shared memory, 78.7 us at 2048 x 16384 (2048 x 12288: 41.9); rows of any length
+// 364 us at 2048 x 28672 bf16, gated (the activation is computed twice, one element a load), 84 at 2048 x 20000 float.
 #include "f8_rowdeal.cuh"
 
 namespace {
