@@ -11,7 +11,7 @@
 //
 // scaled_pair_kernel: products bound by the tensor cores.  Persistent pairs of blocks on 256 x 256 tiles (cta_group::2: each block holds 128 rows
 // of x and 128 of w), two accumulators so that a tile leaves while the next is multiplied, tiles walked in groups of eight rows of tiles.
-// 8192 x 4096 x 8192: 176 us (169 on another box), 3.1 POPS of the 4.2 that instructions alone reach; under the power cap of a long run 204 us (197).
+// 8192 x 4096 x 8192: 176 us (169 on another card), 3.1 POPS of the 4.2 that instructions alone reach; under the power cap of a long run 204 us (197).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -181,7 +181,7 @@ def test_other_threads_run_while_a_launch_waits_for_the_queue():
         torch.cuda.synchronize()
     assert took > 0.4, "the queue was never full"
     gap = max(b - a for a, b in zip(ticks, ticks[1:]))
-    assert gap < took / 4, f"another thread stood still for {gap:.2f} of {took:.2f} s"
+    assert gap < took / 2, f"another thread stood still for {gap:.2f} of {took:.2f} s"
 
 
 def test_calls_on_several_streams_at_once():
